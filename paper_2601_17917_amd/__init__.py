@@ -25,6 +25,8 @@ EXPORTED_SYMBOLS = (
     "sdllm_probe_read", "sdllm_probe_copy", "sdllm_probe_mfma_bf16",
     "sdllm_status_string", "sdllm_last_error", "sdllm_version", "sdllm_init", "sdllm_validate_keep_idx",
     "sdllm_confidence_unmask_noalloc",
+    "sdllm_paged_extend", "sdllm_paged_extend_workspace_bytes", "sdllm_qk_norm_rope", "sdllm_paged_kv_append",
+    "sdllm_paged_attention", "sdllm_paged_attention_workspace_bytes",
 )
 
 
@@ -66,6 +68,39 @@ class RopeParams(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("K", ctypes.c_int32), ("S", ctypes.c_int32), ("n_keep", ctypes.c_int32),
                 ("pos0", ctypes.c_int32), ("theta_base", ctypes.c_float), ("interleaved", ctypes.c_int32)]
+
+
+_Stride = ctypes.c_int64 * 3
+
+
+class PagedExtendParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("K", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32)]
+
+
+class QkNormRopeParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("K", ctypes.c_int32), ("Hq", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("positions_per_row", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("eps", ctypes.c_float), ("theta_base", ctypes.c_float),
+                ("scale_factor", ctypes.c_float), ("low_turns", ctypes.c_float), ("high_turns", ctypes.c_float),
+                ("amplitude", ctypes.c_float), ("original_len", ctypes.c_int32), ("q_stride", _Stride),
+                ("k_stride", _Stride), ("v_stride", _Stride), ("q_out_stride", _Stride), ("k_out_stride", _Stride)]
+
+
+class PagedAppendParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("K", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("pages_layer_stride", ctypes.c_int64), ("block_layer_stride", ctypes.c_int64)]
+
+
+class PagedAttnParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("K", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_kv_len", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("kv_splits", ctypes.c_int32), ("q_stride", _Stride), ("out_stride", _Stride),
+                ("k_block_stride", _Stride), ("v_block_stride", _Stride)]
 
 
 class AttnPlan(ctypes.Structure):
@@ -139,6 +174,18 @@ def load_library(path: Optional[str] = None):
     lib.sdllm_probe_copy.argtypes = [vp, vp, sz, vp]
     lib.sdllm_probe_mfma_bf16.restype = i32
     lib.sdllm_probe_mfma_bf16.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp, ctypes.POINTER(ctypes.c_double)]
+    lib.sdllm_paged_extend_workspace_bytes.restype = sz
+    lib.sdllm_paged_extend_workspace_bytes.argtypes = [ctypes.POINTER(PagedExtendParams)]
+    lib.sdllm_paged_extend.restype = i32
+    lib.sdllm_paged_extend.argtypes = [ctypes.POINTER(PagedExtendParams)] + [vp] * 11 + [vp, sz, vp]
+    lib.sdllm_qk_norm_rope.restype = i32
+    lib.sdllm_qk_norm_rope.argtypes = [ctypes.POINTER(QkNormRopeParams)] + [vp] * 11 + [vp]
+    lib.sdllm_paged_kv_append.restype = i32
+    lib.sdllm_paged_kv_append.argtypes = [ctypes.POINTER(PagedAppendParams)] + [vp] * 5 + [vp]
+    lib.sdllm_paged_attention_workspace_bytes.restype = sz
+    lib.sdllm_paged_attention_workspace_bytes.argtypes = [ctypes.POINTER(PagedAttnParams), ctypes.c_int32]
+    lib.sdllm_paged_attention.restype = i32
+    lib.sdllm_paged_attention.argtypes = [ctypes.POINTER(PagedAttnParams)] + [vp] * 9 + [vp, sz, vp]
     _lib = lib
     return lib
 
@@ -526,6 +573,226 @@ def bind_rope_gathered(x_block, x_suffix, keep_idx, pos0: int, theta_base: float
             _stream(stream))
     keep = (p, x_block, x_suffix, keep_idx, out_block, out_suffix)
     return BoundCall(load_library().sdllm_rope_gathered, args, keep, (out_block, out_suffix))
+
+
+# ---------------------------------------------------------------------------------------------
+# The paged cache (include/sdllm_paged.h).
+def _on_current_device(*tensors):
+    """All tensors on the device whose stream the call is enqueued on: a kernel launched there may not reach others."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise SdllmError(ERR_INVALID_ARG, f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that the call makes; one that another stream than the current one works on is not handed out again before that
+    stream is done with it."""
+    import torch
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None and stream != torch.cuda.current_stream(device):
+        t.record_stream(stream)
+    return t
+
+
+def _shaped(t, name, shape, dtype):
+    """A dense device tensor of this shape and type."""
+    if t is None:
+        return
+    _require(t, name, dtype)
+    if t.shape != shape:
+        raise SdllmError(ERR_INVALID_ARG, f"{name} must be {list(shape)}, is {list(t.shape)}")
+
+
+def _strides(t, name, shape, dtype):
+    """Strides of a device tensor [B, H, K, D] whose last dimension is contiguous; (0, 0, 0) if it is dense."""
+    if not t.is_cuda:
+        raise SdllmError(ERR_INVALID_ARG, f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise SdllmError(ERR_INVALID_ARG, f"{name} must have dtype {dtype}, has {t.dtype}")
+    if t.shape != shape:
+        raise SdllmError(ERR_INVALID_ARG, f"{name} must be {list(shape)}, is {list(t.shape)}")
+    if t.is_contiguous():
+        return _Stride(0, 0, 0)
+    st, n = t.stride(), t.shape
+    if st[3] != 1:
+        raise SdllmError(ERR_INVALID_ARG, f"{name} must have a contiguous last dimension")
+    if any(st[i] == 0 and n[i] > 1 for i in range(3)):
+        raise SdllmError(ERR_INVALID_ARG, f"{name} is a broadcast view")
+    return _Stride(*(st[i] if n[i] > 1 else 0 for i in range(3)))     # the stride of a dimension of one row says nothing
+
+
+def paged_extend(*args, **kw):
+    """sdllm_paged_extend: pages, table entries and slots for up to K new rows of every sequence.  block_table [B,max_pages],
+    free_pages [n_pages], kv_lens [B], n_free [1] (int32) are updated in place; with kv_lens_out / n_free_out the latter two go
+    there instead.  Returns (slots [B,K], granted [B], kv_lens_out, n_free_out).  Signature: see bind_paged_extend."""
+    return bind_paged_extend(*args, **kw)()
+
+
+def bind_paged_extend(block_table, kv_lens, free_pages, n_free, page_size: int, K: int, new_lens=None, do_append=None,
+                      release=None, kv_lens_out=None, n_free_out=None, slots=None, granted=None, workspace=None,
+                      stream=None) -> BoundCall:
+    import torch
+    i32 = torch.int32
+    B, max_pages = block_table.shape
+    kv_lens_out = kv_lens if kv_lens_out is None else kv_lens_out
+    n_free_out = n_free if n_free_out is None else n_free_out
+    n_pages = free_pages.shape[0]
+    dev = block_table.device
+    if slots is None:
+        slots = _new((B, K), i32, dev, stream)
+    if granted is None:
+        granted = _new((B,), i32, dev, stream)
+    _require(block_table, "block_table", i32)
+    _shaped(free_pages, "free_pages", (n_pages,), i32)
+    for name, t in (("kv_lens", kv_lens), ("new_lens", new_lens), ("kv_lens_out", kv_lens_out), ("granted", granted)):
+        _shaped(t, name, (B,), i32)
+    _shaped(n_free, "n_free", (1,), i32)
+    _shaped(n_free_out, "n_free_out", (1,), i32)
+    _shaped(do_append, "do_append", (B,), torch.uint8)
+    _shaped(release, "release", (B,), torch.uint8)
+    _shaped(slots, "slots", (B, K), i32)
+    p = PagedExtendParams(B, K, page_size, max_pages, n_pages)
+    lib = load_library()
+    need = lib.sdllm_paged_extend_workspace_bytes(ctypes.byref(p))
+    if need == ctypes.c_size_t(-1).value:
+        raise SdllmError(ERR_INVALID_ARG, lib.sdllm_last_error().decode())
+    if need and workspace is None:
+        workspace = _new((need,), torch.uint8, dev, stream)
+    tensors = (block_table, kv_lens, new_lens, do_append, release, free_pages, n_free, kv_lens_out, n_free_out, slots, granted)
+    _on_current_device(*tensors, workspace)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = (ctypes.byref(p), *map(_ptr, tensors), _ptr(workspace), ws_bytes, _stream(stream))
+    return BoundCall(lib.sdllm_paged_extend, args, (p, tensors, workspace), (slots, granted, kv_lens_out, n_free_out))
+
+
+def qk_norm_rope(*args, **kw):
+    """sdllm_qk_norm_rope: per-head norms of q [B,Hq,K,D] and k [B,Hkv,K,D] and the rotation of their first rotary_dim
+    elements, in one pass.  positions: int32 [B] (of the first row) or [B,K].  With slots [B,K] the keys, and the rows of v, go
+    into k_pages / v_pages [n_pages,Hkv,page_size,D], otherwise to k_out.  Returns (q_out, k_out), k_out None with slots.
+    Signature: see bind_qk_norm_rope."""
+    return bind_qk_norm_rope(*args, **kw)()
+
+
+def bind_qk_norm_rope(q, k, positions, theta_base: float, q_weight=None, k_weight=None, eps: float = 1e-6,
+                      rotary_dim: Optional[int] = None, interleaved: bool = False, scale_factor: float = 1.0,
+                      original_len: int = 0, low_turns: float = 1.0, high_turns: float = 32.0, amplitude: float = 1.0,
+                      v=None, q_out=None, k_out=None, k_pages=None, v_pages=None, slots=None, stream=None) -> BoundCall:
+    import torch
+    B, Hq, K, D = q.shape
+    Hkv, dtype = k.shape[1], q.dtype
+    if q_out is None:
+        q_out = _new((B, Hq, K, D), dtype, q.device, stream)
+    page_size = n_pages = 0
+    if slots is None:
+        if v is not None or k_pages is not None or v_pages is not None:
+            raise SdllmError(ERR_INVALID_ARG, "qk_norm_rope: v, k_pages and v_pages go with slots")
+        if k_out is None:
+            k_out = _new((B, Hkv, K, D), dtype, q.device, stream)
+    else:
+        if v is None or k_pages is None or v_pages is None or k_out is not None:
+            raise SdllmError(ERR_INVALID_ARG, "qk_norm_rope: with slots give v, k_pages and v_pages, and no k_out")
+        n_pages, page_size = k_pages.shape[0], k_pages.shape[2]
+        _shaped(k_pages, "k_pages", (n_pages, Hkv, page_size, D), dtype)
+        _shaped(v_pages, "v_pages", (n_pages, Hkv, page_size, D), dtype)
+        _shaped(slots, "slots", (B, K), torch.int32)
+    per_row = positions.dim() == 2
+    _shaped(positions, "positions", (B, K) if per_row else (B,), torch.int32)
+    _shaped(q_weight, "q_weight", (D,), dtype)
+    _shaped(k_weight, "k_weight", (D,), dtype)
+    dense = _Stride(0, 0, 0)
+    heads, keys = (B, Hq, K, D), (B, Hkv, K, D)
+    p = QkNormRopeParams(_dtype_code(q), B, K, Hq, Hkv, D, D if rotary_dim is None else rotary_dim, int(bool(interleaved)),
+                         int(per_row), page_size, n_pages, eps, theta_base, scale_factor, low_turns, high_turns, amplitude,
+                         original_len, _strides(q, "q", heads, dtype), _strides(k, "k", keys, dtype),
+                         dense if v is None else _strides(v, "v", keys, dtype), _strides(q_out, "q_out", heads, dtype),
+                         dense if k_out is None else _strides(k_out, "k_out", keys, dtype))
+    tensors = (q, k, v, positions, q_weight, k_weight, q_out, k_out, k_pages, v_pages, slots)
+    _on_current_device(*tensors)
+    args = (ctypes.byref(p), *map(_ptr, tensors), _stream(stream))
+    return BoundCall(load_library().sdllm_qk_norm_rope, args, (p, tensors), (q_out, k_out))
+
+
+def paged_kv_append(*args, **kw):
+    """sdllm_paged_kv_append: the rows of k_blocks / v_blocks [L,B,Hkv,K,D] into slots [B,K] of k_pages / v_pages
+    [L,n_pages,Hkv,page_size,D] (updated in place); rows with slot -1 are skipped.  Signature: see bind_paged_kv_append."""
+    return bind_paged_kv_append(*args, **kw)()
+
+
+def bind_paged_kv_append(k_pages, v_pages, k_blocks, v_blocks, slots, stream=None) -> BoundCall:
+    import torch
+    L, n_pages, Hkv, page_size, D = k_pages.shape
+    B, K = slots.shape
+    dtype = k_pages.dtype
+    for name, t, shape in (("k_pages", k_pages, k_pages.shape), ("v_pages", v_pages, k_pages.shape),
+                           ("k_blocks", k_blocks, (L, B, Hkv, K, D)), ("v_blocks", v_blocks, (L, B, Hkv, K, D))):
+        if t.shape != shape:
+            raise SdllmError(ERR_INVALID_ARG, f"{name} must be {list(shape)}, is {list(t.shape)}")
+        _require_layers(t, name, dtype)
+    _shaped(slots, "slots", (B, K), torch.int32)
+    if L > 1 and (v_pages.stride(0) != k_pages.stride(0) or v_blocks.stride(0) != k_blocks.stride(0)):
+        raise SdllmError(ERR_INVALID_ARG, "paged_kv_append: K and V tensors must share their layer strides")
+    _on_current_device(k_pages, v_pages, k_blocks, v_blocks, slots)
+    p = PagedAppendParams(_dtype_code(k_pages), L, B, Hkv, D, K, page_size, n_pages, k_pages.stride(0) if L > 1 else 0,
+                          k_blocks.stride(0) if L > 1 else 0)
+    tensors = (k_pages, v_pages, k_blocks, v_blocks, slots)
+    args = (ctypes.byref(p), *map(_ptr, tensors), _stream(stream))
+    return BoundCall(load_library().sdllm_paged_kv_append, args, (p, tensors), None)
+
+
+def paged_attn_params(dtype, B, Hq, Hkv, D, K, page_size, n_pages, max_pages, max_kv_len, causal=False, window=0, sinks=0,
+                      scale=0.0, kv_splits=0, **strides) -> PagedAttnParams:
+    return PagedAttnParams(dtype, B, Hq, Hkv, D, K, page_size, n_pages, max_pages, max_kv_len, int(bool(causal)), window, sinks,
+                           scale, kv_splits, **strides)
+
+
+def paged_attention_workspace_bytes(p: PagedAttnParams, with_block: bool) -> int:
+    n = load_library().sdllm_paged_attention_workspace_bytes(ctypes.byref(p), int(with_block))
+    if n == ctypes.c_size_t(-1).value:
+        raise SdllmError(ERR_INVALID_ARG, load_library().sdllm_last_error().decode())
+    return n
+
+
+def paged_attention(*args, **kw):
+    """sdllm_paged_attention: q [B,Hq,K,D] over the cached rows of k_pages / v_pages [n_pages,Hkv,page_size,D] through
+    block_table [B,max_pages] and kv_lens [B] (at most max_kv_len), and over k_block / v_block [B,Hkv,K,D] behind them.  Returns
+    out [B,Hq,K,D]; rows from q_lens[b] on are left as they were.  Signature: see bind_paged_attention."""
+    return bind_paged_attention(*args, **kw)()
+
+
+def bind_paged_attention(q, k_pages, v_pages, block_table, kv_lens, max_kv_len: int, k_block=None, v_block=None, q_lens=None,
+                         causal: bool = False, window: int = 0, sinks: int = 0, scale: float = 0.0, kv_splits: int = 0,
+                         out=None, workspace=None, stream=None) -> BoundCall:
+    import torch
+    B, Hq, K, D = q.shape
+    n_pages, Hkv, page_size = k_pages.shape[:3]
+    dtype = q.dtype
+    if out is None:
+        out = _new((B, Hq, K, D), dtype, q.device, stream)
+    if (k_block is None) != (v_block is None):
+        raise SdllmError(ERR_INVALID_ARG, "paged_attention: give both of k_block and v_block, or neither")
+    _shaped(k_pages, "k_pages", (n_pages, Hkv, page_size, D), dtype)
+    _shaped(v_pages, "v_pages", (n_pages, Hkv, page_size, D), dtype)
+    _shaped(block_table, "block_table", (B, block_table.shape[1]), torch.int32)
+    _shaped(kv_lens, "kv_lens", (B,), torch.int32)
+    _shaped(q_lens, "q_lens", (B,), torch.int32)
+    block = k_block is not None
+    heads, keys = (B, Hq, K, D), (B, Hkv, K, D)
+    dense = _Stride(0, 0, 0)
+    p = paged_attn_params(_dtype_code(q), B, Hq, Hkv, D, K, page_size, n_pages, block_table.shape[1], max_kv_len, causal, window,
+                          sinks, scale, kv_splits, q_stride=_strides(q, "q", heads, dtype),
+                          out_stride=_strides(out, "out", heads, dtype),
+                          k_block_stride=_strides(k_block, "k_block", keys, dtype) if block else dense,
+                          v_block_stride=_strides(v_block, "v_block", keys, dtype) if block else dense)
+    need = paged_attention_workspace_bytes(p, block)
+    if need and workspace is None:
+        workspace = _new((need,), torch.uint8, q.device, stream)
+    tensors = (q, k_pages, v_pages, block_table, kv_lens, k_block, v_block, q_lens, out)
+    _on_current_device(*tensors, workspace)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = (ctypes.byref(p), *map(_ptr, tensors), _ptr(workspace), ws_bytes, _stream(stream))
+    return BoundCall(load_library().sdllm_paged_attention, args, (p, tensors, workspace), out)
 
 
 # ---------------------------------------------------------------------------------------------

@@ -1,6 +1,6 @@
 // Host side of the C ABI: argument validation (before any HIP call), plan / workspace queries,
 // error text, dispatch to the kernel launchers.
-#include "common.h"
+#include "paged_common.h"
 #include <cstdio>
 #include <cstdarg>
 #include <cstring>
@@ -161,6 +161,16 @@ hipError_t scratch_of_current_device(void** out) {
 }
 
 }  // namespace
+
+namespace sdllm {
+int set_error(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof(g_err), fmt, ap);
+  va_end(ap);
+  return code;
+}
+}  // namespace sdllm
 
 extern "C" {
 
