@@ -22,17 +22,12 @@
 //   Online softmax in the log2 domain; a split writes (unnormalised O, m, l) and a second
 //   kernel merges the splits in a fixed order (deterministic, no atomics).
 #include "common.h"
+#include "lds_dma.h"
 #include <algorithm>
 #include <climits>
 #include <type_traits>
 
 namespace sdllm {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
 constexpr int kKeyTile = 64;
 constexpr bool kShareTiles = true;   // 8-wave workgroups with row-split groups for heads with many query rows
@@ -54,90 +49,6 @@ struct AttnArgs {
   int nsplit, tiles_per_split, key_tiles, q_tiles, n_units;
   float scale_log2, inv_scale_log2;
 };
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  // one v_cvt_pk_bf16_f32 (round to nearest even)
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
-}
-
-// One 16-byte-per-lane global -> LDS transfer (the data never passes through registers): lane i's
-// 16 bytes land at lds_addr + 16*i.  Issued through inline assembly so that the compiler's
-// wait-count insertion does not serialise a multi-stage pipeline; completion is tracked by hand
-// with s_waitcnt vmcnt(n) before the workgroup barrier (transfers complete in issue order).
-__device__ __forceinline__ void dma16_sbase(unsigned lds_addr, const void* sbase, unsigned voff) {
-  // the base is the same in every lane; say so, so that it is held in a scalar register pair
-  const unsigned long long p = reinterpret_cast<unsigned long long>(sbase);
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)p);
-  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(p >> 32));
-  const unsigned long long pu = ((unsigned long long)hi << 32) | lo;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(pu) : "memory", "m0");
-}
-// One 16-row slab of one tensor: NT transfers of 1 KiB to consecutive KiB of LDS from one scalar
-// base.  m0 (the LDS base of a transfer) is written once: the instruction's immediate offset moves
-// the LDS address and the global address alike, so transfer j carries offset j KiB and its lane offset
-// voffj has those j KiB taken off beforehand.  One wait state separates the write of m0 from the
-// first transfer that reads it.
-// ONCE: every byte of K/V is read by exactly one workgroup of the launch (one query tile per K/V head and
-// split); the transfers then carry the nontemporal hint (cfg3A 31.1 -> 28.6 us).  Where query tiles share a
-// K/V stream through L2 the hint costs 4-6 %, so it is left off there.
-template <int NT, bool ONCE>
-__device__ __forceinline__ void dma_slab(unsigned lds_addr, const void* sbase, const unsigned (&voffj)[4]) {
-  static_assert(NT == 2 || NT == 4, "transfers per slab");
-  if constexpr (NT == 4 && ONCE)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %2, %1 nt\n\t"
-                 "global_load_lds_dwordx4 %3, %1 offset:1024 nt\n\t"
-                 "global_load_lds_dwordx4 %4, %1 offset:2048 nt\n\t"
-                 "global_load_lds_dwordx4 %5, %1 offset:3072 nt"
-                 :: "s"(lds_addr), "s"(sbase), "v"(voffj[0]), "v"(voffj[1]), "v"(voffj[2]), "v"(voffj[3]) : "memory", "m0");
-  else if constexpr (NT == 4)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %2, %1\n\t"
-                 "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
-                 "global_load_lds_dwordx4 %5, %1 offset:3072"
-                 :: "s"(lds_addr), "s"(sbase), "v"(voffj[0]), "v"(voffj[1]), "v"(voffj[2]), "v"(voffj[3]) : "memory", "m0");
-  else if constexpr (ONCE)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %2, %1 nt\n\t"
-                 "global_load_lds_dwordx4 %3, %1 offset:1024 nt"
-                 :: "s"(lds_addr), "s"(sbase), "v"(voffj[0]), "v"(voffj[1]) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %2, %1\n\t"
-                 "global_load_lds_dwordx4 %3, %1 offset:1024"
-                 :: "s"(lds_addr), "s"(sbase), "v"(voffj[0]), "v"(voffj[1]) : "memory", "m0");
-}
-template <bool ONCE>
-__device__ __forceinline__ void dma16_vaddr(unsigned lds_addr, const void* vaddr) {
-  if constexpr (ONCE)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(vaddr) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(vaddr) : "memory", "m0");
-}
-// A pointer that is the same in every lane, moved into a scalar register pair (64-bit address
-// arithmetic with products is done on the vector ALU; everything derived from the result would
-// otherwise stay there too)
-template <typename T>
-__device__ __forceinline__ const T* uniform_ptr(const T* p) {
-  const unsigned long long v = reinterpret_cast<unsigned long long>(p);
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v);
-  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
-  return reinterpret_cast<const T*>(((unsigned long long)hi << 32) | lo);
-}
-// s_waitcnt vmcnt(n) only (expcnt / lgkmcnt fields left at "no wait")
-template <int N> __device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
-}
 
 // Compile-time shape constants shared by the helpers below (NST = stages of the K/V ring in LDS; NG = 4-wave
 // groups of the workgroup, each of which has a key tile of its own in every stage)
@@ -169,8 +80,6 @@ template <int D> struct Lane {
   unsigned kro[Shape<D>::NS], vro[Shape<D>::NDB];  // LDS read bases (bytes), before compile-time offsets
   unsigned lds_base; int wave, grp, lane, G;        // wave: index within its 4-wave group; grp: the group
 };
-
-typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;   // scalar (constant-cache) loads
 
 // keep_idx values of the first and the last of the 16 rows a wave moves for one key tile, loaded one
 // tile ahead (scalar loads that complete behind the tile being computed).  Indices are clamped, so
@@ -277,8 +186,6 @@ __device__ __forceinline__ void issue_tile(const AttnArgs& a, const Lane<D>& L, 
   }
   load_keep_ahead(a, L.wave, tile + STEP, ka);
 }
-
-typedef s16x4 __attribute__((address_space(3))) * lds_s16x4_ptr;
 
 // V^T operand (16 d x 32 keys) of d block `db`, key half `u`, through two LDS transpose reads
 template <int D, int STAGE, int NG>

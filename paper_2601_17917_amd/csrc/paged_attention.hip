@@ -1,16 +1,8 @@
 // Attention over a paged K/V cache (sdllm_paged_attention): one wave per query row.  Visible keys are [0, sinks) and [lo, hi); a
 // wave takes 64 of them at a time, a lane the score of one, then a lane the output columns.
-#include "paged_common.h"
+#include "paged_attention.h"
 
 namespace sdllm {
-
-struct PagedArgs {
-  const void* q; const void* kp; const void* vp; const int32_t* table; const int32_t* lens;
-  const void* kb; const void* vb; const int32_t* q_lens; void* out;
-  long long q_st[3], o_st[3], kb_st[3], vb_st[3];
-  int B, Hq, Hkv, g, K, shift, n_pages, max_pages, max_kv, causal, window, sinks;
-  float scale;
-};
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((unsigned)x << 16); }
@@ -88,7 +80,11 @@ __global__ __launch_bounds__(256) void paged_attention_row_kernel(PagedArgs a) {
   for (int u = 0; u < D / 64; ++u) store(out + lane + 64 * u, l == 0.f ? 0.f : o[u] / l);
 }
 
-size_t paged_attention_workspace_bytes(const sdllm_paged_attn_params&, bool) { return 0; }
+static bool few_rows(const sdllm_paged_attn_params& p) { return p.dtype == SDLLM_BF16 && (long long)p.Hq / p.Hkv * p.K <= 32; }
+
+size_t paged_attention_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
+  return few_rows(p) ? paged_attention_bf16_workspace_bytes(p, with_block) : 0;
+}
 
 static void dense_or(const int64_t* given, int H, int K, int D, long long* out) {
   const bool dense = given[0] == 0 && given[1] == 0 && given[2] == 0;
@@ -100,16 +96,17 @@ static void dense_or(const int64_t* given, int H, int K, int D, long long* out) 
 hipError_t launch_paged_attention(const sdllm_paged_attn_params& p, const void* q, const void* k_pages, const void* v_pages,
                                   const int32_t* table, const int32_t* lens, const void* k_block, const void* v_block,
                                   const int32_t* q_lens, void* out, void* workspace, hipStream_t stream) {
-  (void)workspace;
   PagedArgs a;
   a.q = q; a.kp = k_pages; a.vp = v_pages; a.table = table; a.lens = lens; a.kb = k_block; a.vb = v_block; a.q_lens = q_lens; a.out = out;
   dense_or(p.q_stride, p.Hq, p.K, p.D, a.q_st);
   dense_or(p.out_stride, p.Hq, p.K, p.D, a.o_st);
   dense_or(p.k_block_stride, p.Hkv, p.K, p.D, a.kb_st);
   dense_or(p.v_block_stride, p.Hkv, p.K, p.D, a.vb_st);
-  a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.shift = __builtin_ctz(p.page_size);
+  a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.R = a.g * p.K; a.shift = __builtin_ctz(p.page_size);
   a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.max_kv = p.max_kv_len; a.causal = p.causal; a.window = p.window; a.sinks = p.sinks;
   a.scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.D);
+  a.scale_log2 = a.scale * kLog2e; a.thr8 = 8.0f / a.scale_log2;
+  if (few_rows(p)) return launch_paged_attention_bf16(p, a, workspace, stream);
   const long long rows = (long long)p.B * p.Hq * p.K;
   const dim3 grid((unsigned)((rows + 3) / 4));
   if (p.dtype == SDLLM_FP32) {

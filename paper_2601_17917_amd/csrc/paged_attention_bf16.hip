@@ -1,0 +1,573 @@
+// bf16 attention over a paged K/V cache for gfx950 (sdllm_paged_attention), few query rows per (sequence, K/V head): one token, a
+// few tokens, a block of up to 32 rows over its heads.
+//
+// Bound by the read of K and V.  Every wave is a stream of its own: it walks a contiguous range of key tiles of the whole call
+// -- sequences, their K/V heads, their tiles, laid end to end -- so that all waves carry the same number of tiles whatever the
+// lengths are, and meets no other wave.  A tile (8 KiB of K and 8 KiB of V) goes global -> LDS into the wave's own 16 KiB, from
+// there into registers in operand layout, and the next tile's transfers go in flight into the same 16 KiB while the products and
+// the softmax of this one run: with eight waves on a CU some 100 KiB are in flight all the time.
+//   S^T = K Q^T, O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, operands laid out as in the dense kernel (rows padded to 16 or 32).
+//   Online softmax: the product's accumulators start at minus the row's reference, so that it yields s - reference and a weight is
+//   one multiply and one exponential, whatever the scores' size; the reference moves only where a maximum exceeds it by 8 in log2
+//   units.
+// A (sequence, head) that one wave walked alone is written at once; of the others every wave leaves (O, m, l), merged in tile order
+// by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
+#include "paged_attention.h"
+
+namespace sdllm {
+
+template <int D> struct StreamShape {
+  static constexpr int TK = 4096 / D;              // keys per tile
+  static constexpr int KB = TK / 16;               // 16-key slabs
+  static constexpr int CPR = D / 8, RPI = 64 / CPR, IPT = 16 / RPI, R256 = 16 / CPR;
+  static constexpr int NS = D / 32, NDB = D / 16, ROWB = D * 2;
+  static constexpr int SLABB = 16 * ROWB, VB = TK * ROWB, WAVEB = 2 * VB;
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Everything in front of these is done before anything behind them: transfers have landed, LDS reads are in registers.  (The
+// waits are the builtin, which the compiler's own wait insertion takes into account; the empty statements keep it from moving
+// memory accesses across.)
+__device__ __forceinline__ void wait_transfers() {
+  asm volatile("" ::: "memory");
+  wait_vmcnt<0>();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
+// Key tiles of each sequence (over one K/V head), and the sum over the batch.  The lanes take 64 sequences at a time.
+template <int TK>
+__device__ __forceinline__ int tiles_of(const PagedArgs& a, int b) {
+  if (b >= a.B) return 0;
+  const Seen s = seen_by(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.K, 0, a.K - 1, TK);
+  return s.q_len > 0 ? max(s.tiles, 1) : 0;        // rows that see nothing are a tile of their own: they are zero
+}
+__device__ __forceinline__ int wave_scan(int v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(v, d);
+    if ((int)(threadIdx.x & 63) >= d) v += up;
+  }
+  return v;
+}
+template <int TK>
+__device__ __forceinline__ long long all_tiles(const PagedArgs& a) {
+  long long total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, b0 + (int)(threadIdx.x & 63))), 63));
+  return total * a.Hkv;
+}
+__device__ __forceinline__ long long tiles_per_worker(const PagedArgs& a, long long total) {
+  const long long n = (total + a.workers - 1) / a.workers;
+  return n > a.min_tiles ? n : a.min_tiles;
+}
+
+// A (sequence, K/V head) being walked; everything uniform
+struct Unit {
+  int b, kvh, i, T;                                // tile i of T
+  Seen s;
+};
+
+template <int TK>
+__device__ __forceinline__ void open_unit(const PagedArgs& a, Unit& u, int b, int kvh, int i) {
+  u.b = b; u.kvh = kvh; u.i = i;
+  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a.lens, q_lens = (const_i32_ptr)(uintptr_t)a.q_lens;
+  u.s = seen_by(a, lens[b], a.q_lens ? q_lens[b] : a.K, 0, a.K - 1, TK);
+  u.T = u.s.q_len > 0 ? max(u.s.tiles, 1) : 0;
+}
+
+// The unit and tile at position f of the call's tiles
+template <int TK>
+__device__ __forceinline__ void locate(const PagedArgs& a, long long f, Unit& u) {
+  const int lane = threadIdx.x & 63;
+  long long before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
+    const int chunk = uniform(__shfl(upto, 63));
+    if (f < before + (long long)chunk * a.Hkv) {
+      const unsigned long long above = __ballot((long long)upto * a.Hkv > f - before);
+      const int l = __builtin_ctzll(above);
+      const int tb = uniform(__shfl(t, l)), first = uniform(__shfl(upto, l)) - tb;
+      const long long rest = f - before - (long long)first * a.Hkv;
+      const int kvh = (int)(rest / tb);
+      open_unit<TK>(a, u, b0 + l, kvh, (int)(rest - (long long)kvh * tb));
+      return;
+    }
+    before += (long long)chunk * a.Hkv;
+  }
+}
+template <int TK>
+__device__ __forceinline__ void next_tile(const PagedArgs& a, Unit& u) {
+  if (++u.i < u.T) return;
+  if (u.kvh + 1 < a.Hkv) { ++u.kvh; u.i = 0; return; }
+  int b = u.b;
+  do { open_unit<TK>(a, u, ++b, 0, 0); } while (u.T == 0 && b + 1 < a.B);
+}
+
+// Where the keys of a tile come from.  `vis`: bit 16 s + r: row r of slab s holds a key that some query row sees (all others are
+// zero in LDS).  Per-lane constants of the transfers: byte offset of the lane's (swizzled) chunk of transfer j minus j KiB.
+template <int D> struct StreamLane {
+  unsigned kgj[4], vgj[4];
+  int rowj[4], kcj[4], vcj[4];                     // row within the slab and byte in the row, for slabs moved row by row
+  unsigned kro[StreamShape<D>::NS], vro[StreamShape<D>::NDB];
+  unsigned base;                                   // LDS address of the wave's area
+};
+
+// Page ids of a tile's slabs (entries past the table's end repeat the last one)
+template <int D>
+__device__ __forceinline__ void load_pages(const PagedArgs& a, const Unit& u, int i, int (&ids)[StreamShape<D>::KB]) {
+  using S = StreamShape<D>;
+  const const_i32_ptr row = (const_i32_ptr)(uintptr_t)(a.table + (long long)u.b * a.max_pages);
+  const int k0 = u.s.tile(i) * S::TK;
+#pragma unroll
+  for (int j = 0; j < S::KB; ++j) ids[j] = row[min((k0 + 16 * j) >> a.shift, a.max_pages - 1)];
+}
+
+template <int D>
+__device__ __forceinline__ unsigned long long issue_tile(const PagedArgs& a, const StreamLane<D>& L, const Unit& u,
+                                                         const int (&ids)[StreamShape<D>::KB], unsigned char* lds_wave) {
+  using S = StreamShape<D>;
+  const Seen& s = u.s;
+  const int lane = threadIdx.x & 63;
+  unsigned long long vis = 0;
+  if (s.tiles == 0) return 0;                      // nothing to see, nothing is read from LDS either
+  const int k0 = s.tile(u.i) * S::TK;
+#pragma unroll
+  for (int j = 0; j < S::KB; ++j) {
+    const int k = k0 + 16 * j;
+    const bool valid = (unsigned)ids[j] < (unsigned)a.n_pages;
+    const long long row0 = (((long long)ids[j] * a.Hkv + u.kvh) << a.shift) + (k & ((1 << a.shift) - 1));
+    if (valid && k + 16 <= s.n && ((k >= s.lo && k + 16 <= s.hi) || k + 16 <= s.sink)) {
+      dma_slab<S::IPT, true>(L.base + j * S::SLABB, uniform_ptr((const unsigned char*)a.kp + row0 * S::ROWB), L.kgj);
+      dma_slab<S::IPT, true>(L.base + S::VB + j * S::SLABB, uniform_ptr((const unsigned char*)a.vp + row0 * S::ROWB), L.vgj);
+      vis |= 0xffffull << (16 * j);
+      continue;
+    }
+    // a border of what is seen, the end of the cache, rows of the block, a page that is not there: row by row, and zeros
+    // where there is no key
+    const int key = k + (lane & 15);
+    const bool seen = key < s.hi && (key >= s.lo || key < s.sink) && (key >= s.n || valid);
+    const unsigned bits = (unsigned)__ballot(seen) & 0xffffu;
+    vis |= (unsigned long long)bits << (16 * j);
+#pragma unroll
+    for (int t = 0; t < S::IPT; ++t) {
+      *reinterpret_cast<u32x4*>(lds_wave + j * S::SLABB + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(lds_wave + S::VB + j * S::SLABB + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
+    }
+    wait_lds();
+#pragma unroll
+    for (int t = 0; t < S::IPT; ++t) {
+      const int r = L.rowj[t];
+      if ((bits >> r) & 1) {
+        const unsigned char *kr, *vr;
+        if (k + r < s.n) {
+          kr = (const unsigned char*)a.kp + (row0 + r) * S::ROWB;
+          vr = (const unsigned char*)a.vp + (row0 + r) * S::ROWB;
+        } else {
+          const long long x = k + r - s.n;
+          kr = (const unsigned char*)a.kb + 2 * (u.b * a.kb_st[0] + u.kvh * a.kb_st[1] + x * a.kb_st[2]);
+          vr = (const unsigned char*)a.vb + 2 * (u.b * a.vb_st[0] + u.kvh * a.vb_st[1] + x * a.vb_st[2]);
+        }
+        dma16_vaddr<true>(L.base + j * S::SLABB + 1024 * t, kr + L.kcj[t]);
+        dma16_vaddr<true>(L.base + S::VB + j * S::SLABB + 1024 * t, vr + L.vcj[t]);
+      }
+    }
+  }
+  return vis;
+}
+
+// Values that are not finite, in a tile whose keys some rows see and others do not: a weight of 0 times such a value would be NaN
+// in the rows that do not see it.  They are taken out (0), and their effect on the rows that see them -- +inf, -inf, NaN -- is
+// found from products of 0 / 1 matrices: which rows see which keys, which keys hold such a value in a column.
+template <int U, int NDB, int RB>
+__device__ __forceinline__ void nonfinite_values(s16x8 (&vop)[U][NDB], const s16x8 (&pk)[RB][U], f32x4 (&o)[RB][NDB]) {
+  bool bad = false;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      const u32x4 x = __builtin_bit_cast(u32x4, vop[u][db]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) bad = bad || (x[w] & 0x7f80u) == 0x7f80u || (x[w] & 0x7f800000u) == 0x7f800000u;
+    }
+  if (__builtin_expect(__ballot(bad) == 0, 1)) return;
+  s16x8 sees[RB][U];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int u = 0; u < U; ++u) sees[rb][u] = pk[rb][u] != 0 ? s16x8(0x3f80) : s16x8(0);
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int kind = 0; kind < 3; ++kind) {         // +inf, -inf, NaN
+      s16x8 has[U];
+      bool any = false;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const s16x8 v = vop[u][db];
+        const s16x8 is = kind == 0 ? (v == (short)0x7f80) : kind == 1 ? (v == (short)0xff80) : ((v & (short)0x7fff) > (short)0x7f80);
+        has[u] = is & (short)0x3f80;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) any = any || has[u][e] != 0;
+      }
+      if (__ballot(any) == 0) continue;
+      const float special = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, has[u]), __builtin_bit_cast(bf16x8, sees[rb][u]), c, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c[e] != 0.f) o[rb][db][e] += special;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) vop[u][db] = has[u] != 0 ? s16x8(0) : vop[u][db];
+    }
+}
+
+template <int D, int RB>
+__global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
+  using S = StreamShape<D>;
+  constexpr int TK = S::TK, KB = S::KB, NS = S::NS, NDB = S::NDB, U = TK / 32;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * S::WAVEB];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, G = lane >> 4;
+  const int wave = uniform(threadIdx.x >> 6);
+  unsigned char* lds_wave = lds + wave * S::WAVEB;
+
+  // this wave's tiles
+  const int worker = blockIdx.x * 4 + wave;
+  if (worker >= a.workers) return;
+  Unit nxt;
+  long long f, f1;
+  if (a.min_tiles == 0) {                          // a wave per (sequence, K/V head)
+    open_unit<TK>(a, nxt, worker / a.Hkv, worker % a.Hkv, 0);
+    f = 0; f1 = nxt.T;
+    if (f1 == 0) return;
+  } else {
+    const long long total = all_tiles<TK>(a), per = tiles_per_worker(a, total);
+    f = worker * per; f1 = f + per < total ? f + per : total;
+    if (f >= f1) return;
+    locate<TK>(a, f, nxt);
+  }
+  int ids[KB];
+  load_pages<D>(a, nxt, nxt.i, ids);
+
+  StreamLane<D> L;
+  L.base = uniform((int)(unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_wave);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int jj = j < S::IPT ? j : 0, r = S::RPI * jj + lane / S::CPR, c = lane % S::CPR;
+    L.rowj[j] = r;
+    L.kcj[j] = (c ^ ((r / S::R256) % S::CPR)) << 4;
+    L.vcj[j] = (c ^ (2 * ((r / S::R256) % (S::CPR / 2)))) << 4;
+    L.kgj[j] = r * S::ROWB + L.kcj[j] - 1024 * jj;
+    L.vgj[j] = r * S::ROWB + L.vcj[j] - 1024 * jj;
+  }
+  {
+    const int fk = (D == 128) ? l16 : (l16 >> 1);
+#pragma unroll
+    for (int s2 = 0; s2 < NS; ++s2) L.kro[s2] = l16 * S::ROWB + (((4 * s2 + G) ^ fk) << 4);
+    const int e4 = l16 >> 2, c4 = l16 & 3;
+    const int fv = (D == 128) ? 2 * (4 * (G & 1) + e4) : 2 * (2 * (G & 1) + (e4 >> 1));
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+      L.vro[db] = S::VB + (4 * G + e4) * S::ROWB + (((2 * db + (c4 >> 1)) ^ fv) << 4) + ((c4 & 1) << 3);
+  }
+  unsigned long long vis_next = issue_tile<D>(a, L, nxt, ids, lds_wave);
+  load_pages<D>(a, nxt, min(nxt.i + 1, nxt.T - 1), ids);
+
+  int part = 0;                                    // of this wave: the first unit's partial result goes to slot 0, the last's to 1
+  while (f < f1) {
+    // ---- a unit: its query rows as MFMA B operands (lane: row l16, d = 32 s + 8 G .. + 7)
+    const Unit cur = nxt;
+    const int begin = cur.i;
+    const int last_row = cur.s.q_len * a.g - 1;
+    bf16x8 qreg[RB][NS];
+    int lo[RB], hi[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int R = min(16 * rb + l16, last_row), r = R / a.g, h = cur.kvh * a.g + R - r * a.g;
+      const uint16_t* qp = (const uint16_t*)a.q + cur.b * a.q_st[0] + h * a.q_st[1] + r * a.q_st[2];
+#pragma unroll
+      for (int s2 = 0; s2 < NS; ++s2) qreg[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
+      row_range(a, cur.s, r, lo[rb], hi[rb]);
+    }
+    // keys that all rows see: up to all_hi, from all_lo on
+    const int all_hi = a.causal ? min(max(cur.s.p0 + 1, 0), cur.s.N) : cur.s.N;
+    const int all_lo = a.window > 0 ? max(cur.s.p1 - a.window + 1, 0) : 0;
+    f32x4 o[RB][NDB];
+    f32x4 neg_m[RB];                               // minus the reference of row l16, in score units, four times
+    float thr[RB], lsum[RB];                       // kNegBig: no reference yet
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      neg_m[rb] = f32x4{0.f, 0.f, 0.f, 0.f}; thr[rb] = kNegBig; lsum[rb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int i = begin;
+    for (; i < cur.T && f < f1; ++i, ++f) {
+      const unsigned long long vis = vis_next;
+      wait_transfers();
+      bf16x8 kop[KB][NS];
+      s16x8 vop[U][NDB];
+      if (cur.s.tiles > 0) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *reinterpret_cast<const bf16x8*>(lds_wave + L.kro[s2] + kb * S::SLABB);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds_wave + L.vro[db] + 32 * u * S::ROWB));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds_wave + L.vro[db] + (32 * u + 16) * S::ROWB));
+            vop[u][db] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+          }
+      }
+      // the operands are in registers: the area takes the next tile
+      wait_lds();
+      if (f + 1 < f1) {
+        next_tile<TK>(a, nxt);
+        if (nxt.i == 0) load_pages<D>(a, nxt, nxt.i, ids);       // a unit's first tile; the others' ids came in ahead
+        vis_next = issue_tile<D>(a, L, nxt, ids, lds_wave);
+        load_pages<D>(a, nxt, min(nxt.i + 1, nxt.T - 1), ids);
+      }
+      if (vis == 0) continue;
+
+      // ---- S^T = K Q^T
+      f32x4 sacc[RB][KB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) sacc[rb][kb] = neg_m[rb];
+#pragma unroll
+      for (int s2 = 0; s2 < NS; ++s2)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+            sacc[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[kb][s2], qreg[rb][s2], sacc[rb][kb], 0, 0, 0);
+      const int k0 = cur.s.tile(i) * TK;
+      constexpr unsigned long long kAll = KB == 4 ? ~0ull : (1ull << (16 * KB)) - 1;
+      const bool masked = vis != kAll || k0 + TK > all_hi || (k0 < all_lo && k0 + TK > a.sinks);
+      if (masked) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = k0 + 16 * kb + 4 * G + e;
+              // (without short circuits: those are branches here)
+              const bool see = (((unsigned)(vis >> (16 * kb)) >> (4 * G + e)) & 1) & (key < hi[rb]) & ((key >= lo[rb]) | (key < a.sinks));
+              sacc[rb][kb][e] = see ? sacc[rb][kb][e] : -INFINITY;
+            }
+      }
+      // ---- online softmax: p = exp2((s - reference) scale_log2)
+      s16x8 pk[RB][U];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+          mx = fmaxf(fmaxf(fmaxf(mx, sacc[rb][kb][0]), fmaxf(sacc[rb][kb][1], sacc[rb][kb][2])), sacc[rb][kb][3]);
+        if (__builtin_amdgcn_ballot_w64(mx > thr[rb]) != 0) {
+          const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+          mx = fmaxf(__uint_as_float(s16[0]), __uint_as_float(s16[1]));
+          const auto s32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+          mx = fmaxf(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
+          const bool move = mx > thr[rb];
+          const float shift = move ? mx : 0.f;
+          const float corr = thr[rb] == kNegBig ? 0.f : exp2_fast(-shift * a.scale_log2);
+          lsum[rb] *= corr;
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) o[rb][db] *= corr;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) sacc[rb][kb] -= shift;
+          neg_m[rb] -= shift;
+          thr[rb] = move ? a.thr8 : thr[rb];
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sacc[rb][kb][e] = exp2_fast(sacc[rb][kb][e] * a.scale_log2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          union { uint32_t w[4]; s16x8 v; } cv;
+          cv.w[0] = pack_bf16x2(sacc[rb][2 * u][0], sacc[rb][2 * u][1]);
+          cv.w[1] = pack_bf16x2(sacc[rb][2 * u][2], sacc[rb][2 * u][3]);
+          cv.w[2] = pack_bf16x2(sacc[rb][2 * u + 1][0], sacc[rb][2 * u + 1][1]);
+          cv.w[3] = pack_bf16x2(sacc[rb][2 * u + 1][2], sacc[rb][2 * u + 1][3]);
+          pk[rb][u] = cv.v;
+        }
+        // row sums on the matrix pipe, from the rounded probabilities that the values are weighted with
+        union { uint32_t w[4]; s16x8 v; } ones;
+        ones.w[0] = ones.w[1] = ones.w[2] = ones.w[3] = 0x3f803f80u;
+        f32x4 ls = {lsum[rb], 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones.v), __builtin_bit_cast(bf16x8, pk[rb][u]), ls, 0, 0, 0);
+        lsum[rb] = ls[0];
+      }
+      if (masked && cur.s.p1 > cur.s.p0) nonfinite_values<U, NDB, RB>(vop, pk, o);
+      // ---- O^T += V^T P^T
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+            o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop[u][db]),
+                                                                __builtin_bit_cast(bf16x8, pk[rb][u]), o[rb][db], 0, 0, 0);
+    }
+
+    // ---- this wave's share of the unit is done
+    const bool whole = begin == 0 && i == cur.T;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int R = 16 * rb + l16;
+      if (R > last_row) continue;
+      if (whole) {
+        const float inv = lsum[rb] == 0.f ? 0.f : 1.0f / lsum[rb];
+        const int r = R / a.g, h = cur.kvh * a.g + R - r * a.g;
+        uint16_t* orow = (uint16_t*)a.out + cur.b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2];
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          uint2 w;
+          w.x = pack_bf16x2(o[rb][db][0] * inv, o[rb][db][1] * inv);
+          w.y = pack_bf16x2(o[rb][db][2] * inv, o[rb][db][3] * inv);
+          *reinterpret_cast<uint2*>(orow + 16 * db + 4 * G) = w;
+        }
+      } else {
+        const long long slot = ((long long)worker * 2 + part) * a.R + R;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(a.ws_o + slot * D + 16 * db + 4 * G) = o[rb][db];
+        if (G == 0) { a.ws_ml[2 * slot] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; a.ws_ml[2 * slot + 1] = lsum[rb]; }
+      }
+    }
+    part = 1;
+  }
+}
+
+// Merges the shares of every output row that several waves walked, in the order of the tiles.  A workgroup per row: 256 / (D / 4)
+// groups of lanes take every so many-th share, then one adds up the groups, in order.
+template <int D>
+__global__ __launch_bounds__(256) void paged_stream_merge_kernel(PagedArgs a) {
+  using S = StreamShape<D>;
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  __shared__ f32x4 o_s[NG][TPR];
+  __shared__ float m_s[NG], l_s[NG];
+  const unsigned unit = blockIdx.x / (unsigned)a.R;
+  const int R = blockIdx.x - unit * a.R, b = unit / (unsigned)a.Hkv, kvh = unit - b * a.Hkv;
+  // where the unit's tiles lie among the call's
+  const int lane = threadIdx.x & 63;
+  long long total = 0, start = 0;
+  int T = 0, q_len = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int t = tiles_of<S::TK>(a, b0 + lane), upto = wave_scan(t);
+    if (b >= b0 && b < b0 + 64) {
+      T = uniform(__shfl(t, b - b0));
+      start = (total + uniform(__shfl(upto, b - b0)) - T) * a.Hkv + (long long)kvh * T;
+    }
+    total += uniform(__shfl(upto, 63));
+  }
+  total *= a.Hkv;
+  q_len = min(max(a.q_lens ? a.q_lens[b] : a.K, 0), a.K);
+  if (T == 0 || R >= q_len * a.g) return;
+  const long long per = tiles_per_worker(a, total);
+  const int w0 = (int)(start / per), w1 = (int)((start + T - 1) / per);
+  if (w0 == w1) return;                            // written by its wave
+  const int grp = threadIdx.x / TPR, d = (threadIdx.x % TPR) * 4;
+  float M = kNegBig, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int w = w0 + grp; w <= w1; w += NG) {
+    // the unit is its wave's first one unless the wave began before it
+    const long long slot = ((long long)w * 2 + (start > w * per ? 1 : 0)) * a.R + R;
+    const f32x4 ov = *reinterpret_cast<const f32x4*>(a.ws_o + slot * D + d);
+    const float mk = a.ws_ml[2 * slot], lk = a.ws_ml[2 * slot + 1];
+    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a.scale_log2), c1 = exp2_fast((mk - up) * a.scale_log2);
+    acc = acc * c0 + ov * c1;
+    l = l * c0 + lk * c1;
+    M = up;
+  }
+  o_s[grp][threadIdx.x % TPR] = acc;
+  if (d == 0) { m_s[grp] = M; l_s[grp] = l; }
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int k = 1; k < NG; ++k) {
+    const float up = fmaxf(M, m_s[k]), c0 = exp2_fast((M - up) * a.scale_log2), c1 = exp2_fast((m_s[k] - up) * a.scale_log2);
+    acc = acc * c0 + o_s[k][threadIdx.x % TPR] * c1;
+    l = l * c0 + l_s[k] * c1;
+    M = up;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const int r = R / a.g, h = kvh * a.g + R - r * a.g;
+  uint2 w2;
+  w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<uint2*>((uint16_t*)a.out + b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2] + d) = w2;
+}
+
+// ---- launch plan, from the parameters alone
+constexpr int kStreamWaves = 8 * kNumCUs;          // resident at once: two workgroups of 64 KiB per CU
+constexpr int kStreamMinTiles = 2;
+constexpr int kStreamMaxRows = 32;
+
+struct StreamPlan { int workers, min_tiles; bool merge; };
+
+static StreamPlan plan_stream(const sdllm_paged_attn_params& p, bool with_block) {
+  const long long TK = 4096 / p.D, units = (long long)p.B * p.Hkv;
+  const long long N = p.max_kv_len + (with_block ? p.K : 0);
+  long long tiles = (N + TK - 1) / TK;             // most a unit can have
+  if (p.window > 0) {
+    const long long seen = (p.window + p.K + TK - 2) / TK + 1 + (p.sinks + TK - 1) / TK;
+    if (seen < tiles) tiles = seen;
+  }
+  if (tiles < 1) tiles = 1;
+  StreamPlan pl;
+  long long per = kStreamMinTiles;
+  if (p.kv_splits > 0) per = (tiles + p.kv_splits - 1) / p.kv_splits;
+  pl.merge = !(p.kv_splits == 1 || units * (p.Hq / p.Hkv) * p.K >= (1 << 24) || (p.kv_splits == 0 && (units >= 2 * kStreamWaves || p.B > 1024 || tiles <= per)));
+  if (!pl.merge) {
+    pl.workers = (int)units; pl.min_tiles = 0;
+    return pl;
+  }
+  pl.min_tiles = (int)per;
+  long long w = (units * tiles + per - 1) / per;
+  const long long most = p.kv_splits > 0 ? 1 << 20 : kStreamWaves;
+  pl.workers = (int)(w < most ? w : most);
+  return pl;
+}
+
+size_t paged_attention_bf16_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
+  const StreamPlan pl = plan_stream(p, with_block);
+  return pl.merge ? (size_t)pl.workers * 2 * (size_t)(p.Hq / p.Hkv) * p.K * (p.D + 2) * sizeof(float) : 0;
+}
+
+template <int D>
+static hipError_t launch_stream(const PagedArgs& a, const StreamPlan& pl, hipStream_t stream) {
+  const dim3 grid((pl.workers + 3) / 4);
+  if (a.R <= 16) hipLaunchKernelGGL((paged_stream_kernel<D, 1>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_stream_kernel<D, 2>), grid, dim3(256), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !pl.merge) return e;
+  hipLaunchKernelGGL(paged_stream_merge_kernel<D>, dim3((unsigned)((long long)a.B * a.Hkv * a.R)), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_attention_bf16(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
+  const StreamPlan pl = plan_stream(p, a.kb != nullptr);
+  a.workers = pl.workers; a.min_tiles = pl.min_tiles;
+  a.ws_o = (float*)workspace;
+  a.ws_ml = a.ws_o ? a.ws_o + (size_t)pl.workers * 2 * a.R * p.D : nullptr;
+  return p.D == 128 ? launch_stream<128>(a, pl, stream) : launch_stream<64>(a, pl, stream);
+}
+
+}  // namespace sdllm

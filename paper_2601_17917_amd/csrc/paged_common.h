@@ -1,14 +1,10 @@
 // Shared by the operators on a paged K/V cache (include/sdllm_paged.h).
 #pragma once
 #include "common.h"
+#include "lds_dma.h"
 #include "sdllm_paged.h"
 
 namespace sdllm {
-
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 // Division of n < 2^31 by a constant 1 <= d < 2^31 with one high multiply (the round-up method: m = ceil(2^32 (2^s - d) / d),
 // s = ceil(log2 d), q = (mulhi(n, m) + n) >> s; the sum stays below 2^32 because mulhi(n, m) <= n).
