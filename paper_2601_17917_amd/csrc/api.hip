@@ -180,6 +180,7 @@ int sdllm_init(void) {
   hipError_t e = sdllm::prepare_attention_bf16();
   if (e == hipSuccess) e = sdllm::prepare_attention_f32();
   if (e == hipSuccess) e = sdllm::prepare_lm_head();
+  if (e == hipSuccess) e = sdllm::prepare_paged_tile();
   void* ptr = nullptr;
   if (e == hipSuccess) e = scratch_of_current_device(&ptr);
   if (e != hipSuccess) return fail(SDLLM_ERR_HIP, "init: %s", hipGetErrorString(e));

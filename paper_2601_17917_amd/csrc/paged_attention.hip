@@ -80,10 +80,11 @@ __global__ __launch_bounds__(256) void paged_attention_row_kernel(PagedArgs a) {
   for (int u = 0; u < D / 64; ++u) store(out + lane + 64 * u, l == 0.f ? 0.f : o[u] / l);
 }
 
-static bool few_rows(const sdllm_paged_attn_params& p) { return p.dtype == SDLLM_BF16 && (long long)p.Hq / p.Hkv * p.K <= 32; }
+static bool few_rows(const sdllm_paged_attn_params& p) { return (long long)p.Hq / p.Hkv * p.K <= 32; }
 
 size_t paged_attention_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
-  return few_rows(p) ? paged_attention_bf16_workspace_bytes(p, with_block) : 0;
+  if (p.dtype == SDLLM_FP32) return 0;
+  return few_rows(p) ? paged_stream_workspace_bytes(p, with_block) : paged_tile_workspace_bytes(p, with_block);
 }
 
 static void dense_or(const int64_t* given, int H, int K, int D, long long* out) {
@@ -106,16 +107,11 @@ hipError_t launch_paged_attention(const sdllm_paged_attn_params& p, const void* 
   a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.max_kv = p.max_kv_len; a.causal = p.causal; a.window = p.window; a.sinks = p.sinks;
   a.scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.D);
   a.scale_log2 = a.scale * kLog2e; a.thr8 = 8.0f / a.scale_log2;
-  if (few_rows(p)) return launch_paged_attention_bf16(p, a, workspace, stream);
+  if (p.dtype == SDLLM_BF16) return few_rows(p) ? launch_paged_stream(p, a, workspace, stream) : launch_paged_tile(p, a, workspace, stream);
   const long long rows = (long long)p.B * p.Hq * p.K;
   const dim3 grid((unsigned)((rows + 3) / 4));
-  if (p.dtype == SDLLM_FP32) {
-    if (p.D == 64) hipLaunchKernelGGL((paged_attention_row_kernel<float, 64>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged_attention_row_kernel<float, 128>), grid, dim3(256), 0, stream, a);
-  } else {
-    if (p.D == 64) hipLaunchKernelGGL((paged_attention_row_kernel<uint16_t, 64>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged_attention_row_kernel<uint16_t, 128>), grid, dim3(256), 0, stream, a);
-  }
+  if (p.D == 64) hipLaunchKernelGGL((paged_attention_row_kernel<float, 64>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((paged_attention_row_kernel<float, 128>), grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -24,90 +24,6 @@ template <int D> struct StreamShape {
   static constexpr int SLABB = 16 * ROWB, VB = TK * ROWB, WAVEB = 2 * VB;
 };
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// Everything in front of these is done before anything behind them: transfers have landed, LDS reads are in registers.  (The
-// waits are the builtin, which the compiler's own wait insertion takes into account; the empty statements keep it from moving
-// memory accesses across.)
-__device__ __forceinline__ void wait_transfers() {
-  asm volatile("" ::: "memory");
-  wait_vmcnt<0>();
-  asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ void wait_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
-  asm volatile("" ::: "memory");
-}
-
-// Key tiles of each sequence (over one K/V head), and the sum over the batch.  The lanes take 64 sequences at a time.
-template <int TK>
-__device__ __forceinline__ int tiles_of(const PagedArgs& a, int b) {
-  if (b >= a.B) return 0;
-  const Seen s = seen_by(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.K, 0, a.K - 1, TK);
-  return s.q_len > 0 ? max(s.tiles, 1) : 0;        // rows that see nothing are a tile of their own: they are zero
-}
-__device__ __forceinline__ int wave_scan(int v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int up = __shfl_up(v, d);
-    if ((int)(threadIdx.x & 63) >= d) v += up;
-  }
-  return v;
-}
-template <int TK>
-__device__ __forceinline__ long long all_tiles(const PagedArgs& a) {
-  long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, b0 + (int)(threadIdx.x & 63))), 63));
-  return total * a.Hkv;
-}
-__device__ __forceinline__ long long tiles_per_worker(const PagedArgs& a, long long total) {
-  const long long n = (total + a.workers - 1) / a.workers;
-  return n > a.min_tiles ? n : a.min_tiles;
-}
-
-// A (sequence, K/V head) being walked; everything uniform
-struct Unit {
-  int b, kvh, i, T;                                // tile i of T
-  Seen s;
-};
-
-template <int TK>
-__device__ __forceinline__ void open_unit(const PagedArgs& a, Unit& u, int b, int kvh, int i) {
-  u.b = b; u.kvh = kvh; u.i = i;
-  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a.lens, q_lens = (const_i32_ptr)(uintptr_t)a.q_lens;
-  u.s = seen_by(a, lens[b], a.q_lens ? q_lens[b] : a.K, 0, a.K - 1, TK);
-  u.T = u.s.q_len > 0 ? max(u.s.tiles, 1) : 0;
-}
-
-// The unit and tile at position f of the call's tiles
-template <int TK>
-__device__ __forceinline__ void locate(const PagedArgs& a, long long f, Unit& u) {
-  const int lane = threadIdx.x & 63;
-  long long before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
-    const int chunk = uniform(__shfl(upto, 63));
-    if (f < before + (long long)chunk * a.Hkv) {
-      const unsigned long long above = __ballot((long long)upto * a.Hkv > f - before);
-      const int l = __builtin_ctzll(above);
-      const int tb = uniform(__shfl(t, l)), first = uniform(__shfl(upto, l)) - tb;
-      const long long rest = f - before - (long long)first * a.Hkv;
-      const int kvh = (int)(rest / tb);
-      open_unit<TK>(a, u, b0 + l, kvh, (int)(rest - (long long)kvh * tb));
-      return;
-    }
-    before += (long long)chunk * a.Hkv;
-  }
-}
-template <int TK>
-__device__ __forceinline__ void next_tile(const PagedArgs& a, Unit& u) {
-  if (++u.i < u.T) return;
-  if (u.kvh + 1 < a.Hkv) { ++u.kvh; u.i = 0; return; }
-  int b = u.b;
-  do { open_unit<TK>(a, u, ++b, 0, 0); } while (u.T == 0 && b + 1 < a.B);
-}
-
 // Where the keys of a tile come from.  `vis`: bit 16 s + r: row r of slab s holds a key that some query row sees (all others are
 // zero in LDS).  Per-lane constants of the transfers: byte offset of the lane's (swizzled) chunk of transfer j minus j KiB.
 template <int D> struct StreamLane {
@@ -178,57 +94,6 @@ __device__ __forceinline__ unsigned long long issue_tile(const PagedArgs& a, con
     }
   }
   return vis;
-}
-
-// Values that are not finite, in a tile whose keys some rows see and others do not: a weight of 0 times such a value would be NaN
-// in the rows that do not see it.  They are taken out (0), and their effect on the rows that see them -- +inf, -inf, NaN -- is
-// found from products of 0 / 1 matrices: which rows see which keys, which keys hold such a value in a column.
-template <int U, int NDB, int RB>
-__device__ __forceinline__ void nonfinite_values(s16x8 (&vop)[U][NDB], const s16x8 (&pk)[RB][U], f32x4 (&o)[RB][NDB]) {
-  bool bad = false;
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      const u32x4 x = __builtin_bit_cast(u32x4, vop[u][db]);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) bad = bad || (x[w] & 0x7f80u) == 0x7f80u || (x[w] & 0x7f800000u) == 0x7f800000u;
-    }
-  if (__builtin_expect(__ballot(bad) == 0, 1)) return;
-  s16x8 sees[RB][U];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-    for (int u = 0; u < U; ++u) sees[rb][u] = pk[rb][u] != 0 ? s16x8(0x3f80) : s16x8(0);
-#pragma unroll
-  for (int db = 0; db < NDB; ++db)
-#pragma unroll
-    for (int kind = 0; kind < 3; ++kind) {         // +inf, -inf, NaN
-      s16x8 has[U];
-      bool any = false;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const s16x8 v = vop[u][db];
-        const s16x8 is = kind == 0 ? (v == (short)0x7f80) : kind == 1 ? (v == (short)0xff80) : ((v & (short)0x7fff) > (short)0x7f80);
-        has[u] = is & (short)0x3f80;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) any = any || has[u][e] != 0;
-      }
-      if (__ballot(any) == 0) continue;
-      const float special = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, has[u]), __builtin_bit_cast(bf16x8, sees[rb][u]), c, 0, 0, 0);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c[e] != 0.f) o[rb][db][e] += special;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) vop[u][db] = has[u] != 0 ? s16x8(0) : vop[u][db];
-    }
 }
 
 template <int D, int RB>
@@ -415,7 +280,33 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
           ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones.v), __builtin_bit_cast(bf16x8, pk[rb][u]), ls, 0, 0, 0);
         lsum[rb] = ls[0];
       }
-      if (masked && cur.s.p1 > cur.s.p0) nonfinite_values<U, NDB, RB>(vop, pk, o);
+      if (masked && cur.s.p1 > cur.s.p0) {         // rows at different positions: what a row does not see must not reach it
+        bool bad = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) bad |= has_nonfinite(__builtin_bit_cast(u32x4, vop[u][db]));
+        if (__builtin_expect(__ballot(bad) != 0, 0)) {
+#pragma unroll 1
+          for (int kind = 0; kind < 3; ++kind)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb) {
+                f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is_kind(vop[u][db], kind)),
+                                                              __builtin_bit_cast(bf16x8, weighed(pk[rb][u])), c, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[rb][db][e] += c[e] != 0.f ? of_kind(kind) : 0.f;
+              }
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) vop[u][db] = finite_part(vop[u][db]);
+        }
+      }
       // ---- O^T += V^T P^T
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -455,11 +346,10 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
   }
 }
 
-// Merges the shares of every output row that several waves walked, in the order of the tiles.  A workgroup per row: 256 / (D / 4)
+// Merges the shares of every output row that several workers (waves here, workgroups of the tile kernel) walked, in the order of the tiles.  A workgroup per row: 256 / (D / 4)
 // groups of lanes take every so many-th share, then one adds up the groups, in order.
-template <int D>
-__global__ __launch_bounds__(256) void paged_stream_merge_kernel(PagedArgs a) {
-  using S = StreamShape<D>;
+template <int D, int TK>
+__global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs a) {
   constexpr int TPR = D / 4, NG = 256 / TPR;
   __shared__ f32x4 o_s[NG][TPR];
   __shared__ float m_s[NG], l_s[NG];
@@ -470,7 +360,7 @@ __global__ __launch_bounds__(256) void paged_stream_merge_kernel(PagedArgs a) {
   long long total = 0, start = 0;
   int T = 0, q_len = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int t = tiles_of<S::TK>(a, b0 + lane), upto = wave_scan(t);
+    const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
     if (b >= b0 && b < b0 + 64) {
       T = uniform(__shfl(t, b - b0));
       start = (total + uniform(__shfl(upto, b - b0)) - T) * a.Hkv + (long long)kvh * T;
@@ -546,9 +436,17 @@ static StreamPlan plan_stream(const sdllm_paged_attn_params& p, bool with_block)
   return pl;
 }
 
-size_t paged_attention_bf16_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
+size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
   const StreamPlan pl = plan_stream(p, with_block);
   return pl.merge ? (size_t)pl.workers * 2 * (size_t)(p.Hq / p.Hkv) * p.K * (p.D + 2) * sizeof(float) : 0;
+}
+
+hipError_t launch_shares_merge(const PagedArgs& a, int D, int TK, hipStream_t stream) {
+  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.R));
+  if (D == 64) hipLaunchKernelGGL((shares_merge_kernel<64, 64>), grid, dim3(256), 0, stream, a);
+  else if (TK == 32) hipLaunchKernelGGL((shares_merge_kernel<128, 32>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((shares_merge_kernel<128, 64>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 template <int D>
@@ -558,11 +456,10 @@ static hipError_t launch_stream(const PagedArgs& a, const StreamPlan& pl, hipStr
   else hipLaunchKernelGGL((paged_stream_kernel<D, 2>), grid, dim3(256), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !pl.merge) return e;
-  hipLaunchKernelGGL(paged_stream_merge_kernel<D>, dim3((unsigned)((long long)a.B * a.Hkv * a.R)), dim3(256), 0, stream, a);
-  return hipGetLastError();
+  return launch_shares_merge(a, D, 4096 / D, stream);
 }
 
-hipError_t launch_paged_attention_bf16(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
+hipError_t launch_paged_stream(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
   const StreamPlan pl = plan_stream(p, a.kb != nullptr);
   a.workers = pl.workers; a.min_tiles = pl.min_tiles;
   a.ws_o = (float*)workspace;
