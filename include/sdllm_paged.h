@@ -146,7 +146,7 @@ int sdllm_paged_kv_append(const sdllm_paged_append_params* p,
  *
  *   B, Hq, Hkv, D   as for sdllm_block_attention; D in {64, 128} for both dtypes; B * Hkv < 2^22
  *   K               query rows per sequence of q, out and the block (>= 1)
- *   page_size, n_pages, max_pages (entries of a table row, > 0)
+ *   page_size, n_pages, max_pages (entries of a table row, > 0); a page of all heads below 2 GiB
  *   max_kv_len      upper bound of kv_lens, <= max_pages * page_size: the launch plan is made for it (the lengths themselves are
  *                   device data); max_kv_len + K <= 2^30
  *   scale           softmax scale; <= 0 selects 1/sqrt(D)

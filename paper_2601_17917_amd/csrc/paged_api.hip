@@ -128,6 +128,7 @@ int check_paged_attn(const sdllm_paged_attn_params* p, bool with_block) {
       rows * p->B > 0x7fffffffLL || (long long)p->B * p->max_pages > 0x7fffffffLL)
     return set_error(kUnsupported, "%s: sequence or batch too large", w);
   const int e = p->dtype == SDLLM_FP32 ? 4 : 2;
+  if ((long long)p->Hkv * p->page_size * p->D * e >= (1LL << 31)) return set_error(kUnsupported, "%s: a page of all heads must be below 2 GiB", w);
   if (int rc = check_strides(w, "q", p->q_stride, p->B, p->Hq, p->K, p->D, e, false)) return rc;
   if (int rc = check_strides(w, "out", p->out_stride, p->B, p->Hq, p->K, p->D, e, true)) return rc;
   if (with_block) {

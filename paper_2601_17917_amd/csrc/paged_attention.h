@@ -11,9 +11,19 @@ struct PagedArgs {
   long long q_st[3], o_st[3], kb_st[3], vb_st[3];  // elements
   int B, Hq, Hkv, g, K, R;                         // R = g K: query rows of a (sequence, K/V head)
   int shift, n_pages, max_pages, max_kv, causal, window, sinks;
-  int workers, parts, row_tiles, min_tiles;        // how the key tiles are shared out (see the kernels)
+  unsigned page_bytes;                             // of one page, all heads
+  int workers, parts, row_tiles, cuts, min_tiles;  // how the key tiles are shared out (see the kernels)
   float scale, scale_log2, thr8;                    // thr8: 8 in log2 units, as a difference of scores
 };
+
+// The kernels read their arguments where they use them: a fresh pointer that the compiler cannot see through, in a scope of its own,
+// keeps what a unit's start and end need out of the registers of the loop between them.
+typedef const __attribute__((address_space(4))) PagedArgs* Args;
+__device__ __forceinline__ Args arguments() {
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegBig = -3.0e38f;
@@ -29,32 +39,41 @@ struct Seen {
   int p0, p1;                                      // positions of the first and the last row
   int lo, hi, sink;
   int sink_tiles, first, tiles;
+  int last16, sink16;                              // 16 keys from k on are cached and seen if lo <= k <= last16, or k <= sink16
   __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : first + i - sink_tiles; }
 };
 
-__device__ __forceinline__ Seen seen_by(const PagedArgs& a, int n, int q_len, int r0, int r1, int TK) {
+__device__ __forceinline__ Seen seen_by(Args a, int n, int q_len, int r0, int r1, int TK) {
   Seen s;
-  s.n = min(max(n, 0), a.max_kv);
-  s.q_len = min(max(q_len, 0), a.K);
-  s.N = s.n + (a.kb != nullptr ? s.q_len : 0);
+  s.n = min(max(n, 0), a->max_kv);
+  s.q_len = min(max(q_len, 0), a->K);
+  s.N = s.n + (a->kb != nullptr ? s.q_len : 0);
   s.p0 = s.N - s.q_len + r0;
   s.p1 = s.N - s.q_len + min(r1, s.q_len - 1);
-  s.hi = a.causal ? min(max(s.p1 + 1, 0), s.N) : s.N;
-  s.lo = a.window > 0 ? min(max(s.p0 - a.window + 1, 0), s.hi) : 0;
-  s.sink = min(a.sinks, s.lo);
+  s.hi = a->causal ? min(max(s.p1 + 1, 0), s.N) : s.N;
+  s.lo = a->window > 0 ? min(max(s.p0 - a->window + 1, 0), s.hi) : 0;
+  s.sink = min(a->sinks, s.lo);
+  s.last16 = min(s.n, s.hi) - 16;
   s.first = s.lo / TK;
+  s.sink16 = min(s.n, s.sink) - 16;
   s.sink_tiles = min((s.sink + TK - 1) / TK, s.first);
   s.tiles = s.sink_tiles + (s.hi + TK - 1) / TK - s.first;       // lo < hi unless both are 0: then none
   return s;
 }
 
 // Keys visible to row r of the tile: [lo, hi) and below sinks
-__device__ __forceinline__ void row_range(const PagedArgs& a, const Seen& s, int r, int& lo, int& hi) {
+__device__ __forceinline__ void row_range(Args a, const Seen& s, int r, int& lo, int& hi) {
   const int p = s.N - s.q_len + r;
-  hi = a.causal ? min(max(p + 1, 0), s.N) : s.N;
-  lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
+  hi = a->causal ? min(max(p + 1, 0), s.N) : s.N;
+  lo = a->window > 0 ? max(p - a->window + 1, 0) : 0;
 }
 
+// The lane, made anew: what a slower path derives from it is not kept in registers over the loop
+__device__ __forceinline__ int fresh_lane() {
+  int x = threadIdx.x;
+  asm volatile("" : "+v"(x));
+  return x & 63;
+}
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Everything in front of these is done before anything behind them: transfers have landed, LDS reads are in registers.  (The
@@ -73,9 +92,9 @@ __device__ __forceinline__ void wait_lds() {
 
 // Key tiles of each sequence (over one K/V head), and the sum over the batch.  The lanes take 64 sequences at a time.
 template <int TK>
-__device__ __forceinline__ int tiles_of(const PagedArgs& a, int b) {
-  if (b >= a.B) return 0;
-  const Seen s = seen_by(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.K, 0, a.K - 1, TK);
+__device__ __forceinline__ int tiles_of(Args a, int b) {
+  if (b >= a->B) return 0;
+  const Seen s = seen_by(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, 0, a->K - 1, TK);
   return s.q_len > 0 ? max(s.tiles, 1) : 0;        // rows that see nothing are a tile of their own: they are zero
 }
 __device__ __forceinline__ int wave_scan(int v) {
@@ -87,14 +106,14 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 template <int TK>
-__device__ __forceinline__ long long all_tiles(const PagedArgs& a) {
+__device__ __forceinline__ long long all_tiles(Args a) {
   long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, b0 + (int)(threadIdx.x & 63))), 63));
-  return total * a.Hkv;
+  for (int b0 = 0; b0 < a->B; b0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, b0 + (int)(threadIdx.x & 63))), 63));
+  return total * a->Hkv;
 }
-__device__ __forceinline__ long long tiles_per_worker(const PagedArgs& a, long long total) {
-  const long long n = (total + a.workers - 1) / a.workers;
-  return n > a.min_tiles ? n : a.min_tiles;
+__device__ __forceinline__ long long tiles_per_worker(Args a, long long total) {
+  const long long n = (total + a->workers - 1) / a->workers;
+  return n > a->min_tiles ? n : a->min_tiles;
 }
 
 // A (sequence, K/V head) being walked; everything uniform
@@ -104,59 +123,300 @@ struct Unit {
 };
 
 template <int TK>
-__device__ __forceinline__ void open_unit(const PagedArgs& a, Unit& u, int b, int kvh, int i) {
+__device__ __forceinline__ void open_unit(Unit& u, int b, int kvh, int i) {
+  const Args a = arguments();
   u.b = b; u.kvh = kvh; u.i = i;
-  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a.lens, q_lens = (const_i32_ptr)(uintptr_t)a.q_lens;
-  u.s = seen_by(a, lens[b], a.q_lens ? q_lens[b] : a.K, 0, a.K - 1, TK);
+  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
+  u.s = seen_by(a, lens[b], a->q_lens ? q_lens[b] : a->K, 0, a->K - 1, TK);
   u.T = u.s.q_len > 0 ? max(u.s.tiles, 1) : 0;
 }
 
-// The unit and tile at position f of the call's tiles
+// The unit and tile that the share of worker w begins with; returns the tiles of the share (0: none)
 template <int TK>
-__device__ __forceinline__ void locate(const PagedArgs& a, long long f, Unit& u) {
+__device__ __forceinline__ int open_share(int w, Unit& u) {
+  const Args a = arguments();
   const int lane = threadIdx.x & 63;
+  const long long total = all_tiles<TK>(a), per = tiles_per_worker(a, total), f = w * per;
+  if (f >= total) return 0;
   long long before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
+  for (int b0 = 0; b0 < a->B; b0 += 64) {
     const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
     const int chunk = uniform(__shfl(upto, 63));
-    if (f < before + (long long)chunk * a.Hkv) {
-      const unsigned long long above = __ballot((long long)upto * a.Hkv > f - before);
+    if (f < before + (long long)chunk * a->Hkv) {
+      const unsigned long long above = __ballot((long long)upto * a->Hkv > f - before);
       const int l = __builtin_ctzll(above);
       const int tb = uniform(__shfl(t, l)), first = uniform(__shfl(upto, l)) - tb;
-      const long long rest = f - before - (long long)first * a.Hkv;
+      const long long rest = f - before - (long long)first * a->Hkv;
       const int kvh = (int)(rest / tb);
-      open_unit<TK>(a, u, b0 + l, kvh, (int)(rest - (long long)kvh * tb));
-      return;
+      open_unit<TK>(u, b0 + l, kvh, (int)(rest - (long long)kvh * tb));
+      break;
     }
-    before += (long long)chunk * a.Hkv;
+    before += (long long)chunk * a->Hkv;
   }
+  return (int)(per < total - f ? per : total - f);
 }
 template <int TK>
-__device__ __forceinline__ void next_tile(const PagedArgs& a, Unit& u) {
+__device__ __forceinline__ void next_tile(Unit& u) {
   if (++u.i < u.T) return;
-  if (u.kvh + 1 < a.Hkv) { ++u.kvh; u.i = 0; return; }
+  const Args a = arguments();
+  if (u.kvh + 1 < a->Hkv) { ++u.kvh; u.i = 0; return; }
   int b = u.b;
-  do { open_unit<TK>(a, u, ++b, 0, 0); } while (u.T == 0 && b + 1 < a.B);
+  do { open_unit<TK>(u, ++b, 0, 0); } while (u.T == 0 && b + 1 < a->B);
 }
 
-// Values that are not finite, in a tile whose keys some rows see and others do not: a weight of 0 times such a value would be NaN
-// in the rows that do not see it.  They are taken out of the product (0), and their effect on the rows that see them -- +inf, -inf,
-// NaN -- is found from products of 0 / 1 matrices: which rows see which keys, which keys hold such a value in a column.
-__device__ __forceinline__ bool has_nonfinite(const u32x4& x) {      // eight bf16
-  bool bad = false;
+// What the loop over tiles needs of the arguments
+struct Hot {
+  const unsigned char* kp; const unsigned char* vp;
+  unsigned page_bytes; int n_pages, shift, last_page, window, sinks;
+  float scale_log2, thr8;
+};
+__device__ __forceinline__ Hot hot_arguments() {
+  const Args a = arguments();
+  Hot h;
+  h.kp = (const unsigned char*)a->kp; h.vp = (const unsigned char*)a->vp;
+  h.page_bytes = a->page_bytes; h.n_pages = a->n_pages; h.shift = a->shift; h.last_page = a->max_pages - 1; h.sinks = a->sinks; h.window = a->window;
+  h.scale_log2 = a->scale_log2; h.thr8 = a->thr8;
+  // each in a register of its own, not a part of the tuples they were loaded in
+  asm volatile("" : "+s"(h.kp), "+s"(h.vp), "+s"(h.page_bytes), "+s"(h.n_pages), "+s"(h.shift), "+s"(h.last_page), "+s"(h.sinks), "+s"(h.window),
+               "+s"(h.scale_log2), "+s"(h.thr8));
+  return h;
+}
+// The 64 entries of a sequence's block table around the current tile, one per lane: a tile's page ids are lane reads, and memory is
+// only asked again 64 pages further on.  (A scalar load per tile would make every LDS wait behind it a wait for it, too.)
+struct Pages {
+  const int32_t* row;                              // of the sequence
+  int block, id;                                   // entry 64 block + lane
+  unsigned long long valid;                        // which of them are pages of the pool
+  __device__ __forceinline__ void open(int b) {
+    const Args a = arguments();
+    row = a->table + (long long)b * a->max_pages;
+    block = -1;
+  }
+  __device__ __forceinline__ void seek(const Hot& h, int k) {          // to the tile at key k
+    const int want = k >> (h.shift + 6);
+    if (want == block) return;
+    block = want;
+    id = row[min(64 * want + fresh_lane(), h.last_page)];   // entries behind the table's end repeat the last one
+    valid = __ballot((unsigned)id < (unsigned)h.n_pages);
+  }
+  __device__ __forceinline__ int of(const Hot& h, int k) const { return __builtin_amdgcn_readlane(id, (k >> h.shift) & 63); }
+  __device__ __forceinline__ bool ok(const Hot& h, int k) const { return (valid >> ((k >> h.shift) & 63)) & 1; }
+  // all pages of the TK keys from k on (a multiple of TK)
+  template <int TK> __device__ __forceinline__ bool all_ok(const Hot& h, int k) const {
+    const int n = TK >> h.shift;                   // pages of the tile, if more than one
+    const unsigned long long want = n > 1 ? (1ull << n) - 1 : 1;
+    return ((valid >> ((k >> h.shift) & 63)) & want) == want;
+  }
+};
+// Byte offset in kp / vp of row k of K/V head kvh, which lies in page id
+__device__ __forceinline__ unsigned long long row_offset(const Hot& h, int id, int kvh, int k, int row_bytes) {
+  return (unsigned long long)(unsigned)id * h.page_bytes + (unsigned)(((kvh << h.shift) + (k & ((1 << h.shift) - 1))) * row_bytes);
+}
+
+// ---- K/V rows global -> LDS, in slabs of 16 rows.  LDS rows are unpadded; 16-byte chunk c of row r lies at c ^ f(r), f_K(r) = (r / R256)
+// mod CPR, f_V(r) = 2 ((r / R256) mod (CPR / 2)), which keeps the operand reads free of bank conflicts (as in the dense kernel).
+template <int D> struct Slab {
+  static constexpr int CPR = D / 8;                // chunks per row
+  static constexpr int RPI = 64 / CPR;             // rows per wave-wide transfer
+  static constexpr int IPT = 16 / RPI;             // transfers per slab
+  static constexpr int R256 = 16 / CPR;            // rows per 256 bytes
+  static constexpr int ROWB = D * 2, BYTES = 16 * ROWB;
+  // byte within the source of the lane's chunk of transfer 0, and the bits of it that transfer j flips (less j KiB, dma_slab)
+  __device__ static unsigned lane_offset(bool v) {
+    const int lane = fresh_lane(), r = lane / CPR, c = lane % CPR;
+    return r * ROWB + ((c ^ (v ? 2 * ((r / R256) % (CPR / 2)) : (r / R256) % CPR)) << 4);
+  }
+  __device__ static constexpr unsigned flips(bool v, int j) { return v ? (D == 128 ? 128 * (j & 1) : 0) : 64 * j; }
+};
+
+// Whole slab from consecutive rows; V: which tensor's order.  (The offsets are made here: kept over a loop they cost registers.)
+template <int D, bool ONCE, bool V>
+__device__ __forceinline__ void move_slab(unsigned lds, const unsigned char* src) {
+  const unsigned g = Slab<D>::lane_offset(V);
+  const unsigned off[4] = {g, g ^ Slab<D>::flips(V, 1), g ^ Slab<D>::flips(V, 2), g ^ Slab<D>::flips(V, 3)};
+  dma_slab<Slab<D>::IPT, ONCE>(lds, uniform_ptr(src), off);
+}
+
+// Whole slab from 16 rows `stride` bytes apart (a block's rows as a projection leaves them)
+template <int D, bool ONCE, bool V>
+__device__ __forceinline__ void move_strided(unsigned lds, const unsigned char* src, unsigned stride) {
+  using S = Slab<D>;
+  const int lane = fresh_lane(), c = lane % S::CPR;
+  unsigned off[4];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) bad |= ((x[w] & 0x7f80u) == 0x7f80u) | ((x[w] & 0x7f800000u) == 0x7f800000u);
-  return bad;
+  for (int j = 0; j < 4; ++j) {
+    const int r = S::RPI * (j < S::IPT ? j : 0) + lane / S::CPR;
+    off[j] = r * stride + ((c ^ (V ? 2 * ((r / S::R256) % (S::CPR / 2)) : (r / S::R256) % S::CPR)) << 4) - 1024 * (j < S::IPT ? j : 0);
+  }
+  dma_slab<S::IPT, ONCE>(lds, uniform_ptr(src), off);
 }
-__device__ __forceinline__ s16x8 finite_part(const s16x8& v) { return ((v & (short)0x7f80) == (short)0x7f80) ? s16x8(0) : v; }
-// 1 where v is +inf (kind 0), -inf (1), NaN (2); kind is uniform
-__device__ __forceinline__ s16x8 is_kind(const s16x8& v, int kind) {
-  const s16x8 nan = (v & (short)0x7fff) > (short)0x7f80, inf = v == (short)(kind == 0 ? 0x7f80 : 0xff80);
-  return (kind == 2 ? nan : inf) & (short)0x3f80;
+// The block's rows of a (sequence, K/V head)
+struct BlockRows {
+  const unsigned char *k, *v;                      // of row 0
+  unsigned k_stride, v_stride;                     // bytes between rows; 0: no block, or too far apart for an offset of 32 bits
+  __device__ __forceinline__ void open(int b, int kvh) {
+    const Args a = arguments();
+    k_stride = v_stride = 0;
+    k = v = nullptr;
+    if (a->kb == nullptr || a->kb_st[2] >= (1 << 26) || a->vb_st[2] >= (1 << 26)) return;
+    k = (const unsigned char*)a->kb + 2 * (b * a->kb_st[0] + kvh * a->kb_st[1]);
+    v = (const unsigned char*)a->vb + 2 * (b * a->vb_st[0] + kvh * a->vb_st[1]);
+    k_stride = (unsigned)(2 * a->kb_st[2]); v_stride = (unsigned)(2 * a->vb_st[2]);
+  }
+};
+
+// Which of the TK keys from k on (a multiple of 16) some query row sees and has a page: bit r: key k + r
+template <int TK>
+__device__ __forceinline__ unsigned long long seen_keys(const Hot& h, const Seen& s, const Pages& p, int k) {
+  const int lane = fresh_lane(), key = k + lane;
+  bool page = false;
+#pragma unroll
+  for (int j = 0; j < TK / 16; ++j) page |= (lane >> 4) == j && p.ok(h, k + 16 * j);
+  return __ballot((lane < TK) & (key < s.hi) & ((key >= s.lo) | (key < s.sink)) & ((key >= s.n) | page));
 }
-__device__ __forceinline__ float of_kind(int kind) { return kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf(""); }
-// 1 where a weight is not zero
-__device__ __forceinline__ s16x8 weighed(const s16x8& p) { return p != 0 ? s16x8(0x3f80) : s16x8(0); }
+
+// Rows of a slab from wherever they lie, zeros for those whose bit is not set.  page_row: address of key k in its page.
+template <int D, bool ONCE, bool V>
+__device__ __forceinline__ void move_rows(const Seen& s, int b, int kvh, int k, unsigned bits, const unsigned char* page_row, unsigned lds,
+                                          unsigned char* lds_ptr) {
+  using S = Slab<D>;
+  const int lane = fresh_lane(), c = lane % S::CPR;
+#pragma unroll
+  for (int t = 0; t < S::IPT; ++t) *reinterpret_cast<u32x4*>(lds_ptr + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
+  wait_lds();
+  if (bits == 0) return;
+  const Args a = arguments();
+  const unsigned char* block = (const unsigned char*)(V ? a->vb : a->kb);
+  const long long st = V ? a->vb_st[2] : a->kb_st[2];
+  if (block != nullptr) block += 2 * (b * (V ? a->vb_st[0] : a->kb_st[0]) + kvh * (V ? a->vb_st[1] : a->kb_st[1]) + (k - s.n) * st);
+#pragma unroll 1
+  for (int t = 0; t < S::IPT; ++t) {
+    const int r = S::RPI * t + lane / S::CPR;
+    const int at = (c ^ (V ? 2 * ((r / S::R256) % (S::CPR / 2)) : (r / S::R256) % S::CPR)) << 4;
+    if ((bits >> r) & 1) dma16_vaddr<ONCE>(lds + 1024 * t, (k + r < s.n ? page_row + r * S::ROWB : block + 2 * r * st) + at);
+  }
+}
+
+// Scores of hidden keys become -inf.  Score [kb][e] of a lane is key k0 + 16 kb + 4 G + e of its row, which sees keys [lo, hi) and
+// those below sinks; bit 16 kb + 4 G + e of vis: the key exists.  Border by border: most tiles that have one have one kind.
+template <int KB>
+__device__ __forceinline__ void hide(f32x4 (&z)[KB], int k0, int lo, int hi, int sinks, unsigned long long vis, bool some_missing,
+                                     bool above, bool below) {
+  const int G4 = (fresh_lane() >> 4) * 4;
+  if (some_missing) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const unsigned bits = (unsigned)(vis >> (16 * kb)) >> G4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[kb][e] = (bits >> e) & 1 ? z[kb][e] : -INFINITY;
+    }
+  }
+  if (above) {
+    const int t = hi - k0 - G4;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[kb][e] = 16 * kb + e < t ? z[kb][e] : -INFINITY;
+  }
+  if (below) {
+    const int t = lo - k0 - G4, u = sinks - k0 - G4;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[kb][e] = ((16 * kb + e >= t) | (16 * kb + e < u)) ? z[kb][e] : -INFINITY;
+  }
+}
+
+// ---- Values that are not finite, in a tile whose keys some rows see and others do not: a weight of 0 times such a value would be NaN
+// in the rows that do not see it.  The kernels look for them in such tiles only, take them as 0 there, and have the rows that see
+// one computed again at the end (redo_rows).
+// Bits 15 and 31 of the result: one of the low / high bf16 of x has an exponent of all ones.
+__device__ __forceinline__ unsigned nonfinite_bits(const u32x4& x) {
+  unsigned bad = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) bad |= (x[w] & 0x7f807f80u) + 0x00800080u;
+  return bad & 0x80008000u;
+}
+__device__ __forceinline__ s16x8 finite_part(const s16x8& v) {
+  u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const unsigned bad = ((x[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    x[w] &= ~(bad - (bad >> 15));                  // 0x7fff in the halves to clear: +0 or -0
+  }
+  return __builtin_bit_cast(s16x8, x);
+}
+
+// Rows R0 .. R0 + count - 1 of a unit over its tiles [i0, i1), one row after the other: a lane per key, then a lane per column.  Where the
+// result is finite, what the caller has written stands; else it is written again, as a row of the output or as a partial result.
+template <int D, int TK>
+__device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0, int i1, int R0, int count, bool whole,
+                                          long long slot0) {
+  const Args a = arguments();
+  const int lane = threadIdx.x & 63;
+  wait_transfers();                                // what the caller has written is in front of what is written here
+#pragma unroll 1
+  for (int R = R0; R < min(R0 + count, s.q_len * a->g); ++R) {
+    const int r = R / a->g, h = kvh * a->g + R - r * a->g;
+    const uint16_t* q = (const uint16_t*)a->q + b * a->q_st[0] + h * a->q_st[1] + r * a->q_st[2];
+    int lo, hi;
+    row_range(a, s, r, lo, hi);
+    float m = kNegBig, l = 0.f, o[D / 64] = {};
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+      const int key = s.tile(i) * TK + lane;
+      bool sees = (lane < TK) & (key < hi) & ((key >= lo) | (key < a->sinks));
+      const uint16_t *k = nullptr, *v = nullptr;
+      if (sees) {
+        if (key < s.n) {
+          const int page = a->table[(long long)b * a->max_pages + (key >> a->shift)];
+          sees = (unsigned)page < (unsigned)a->n_pages;
+          const long long at = ((((long long)page * a->Hkv + kvh) << a->shift) + (key & ((1 << a->shift) - 1))) * D;
+          k = (const uint16_t*)a->kp + at; v = (const uint16_t*)a->vp + at;
+        } else {
+          k = (const uint16_t*)a->kb + b * a->kb_st[0] + kvh * a->kb_st[1] + (key - s.n) * a->kb_st[2];
+          v = (const uint16_t*)a->vb + b * a->vb_st[0] + kvh * a->vb_st[1] + (key - s.n) * a->vb_st[2];
+        }
+      }
+      float z = -INFINITY;
+      if (sees) {
+        z = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; ++d) z = fmaf(__uint_as_float((unsigned)q[d] << 16), __uint_as_float((unsigned)k[d] << 16), z);
+      }
+      float mx = z;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+      const float up = fmaxf(m, mx), corr = exp2_fast((m - up) * a->scale_log2), p = exp2_fast((z - up) * a->scale_log2);
+      float sum = p;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+      m = up; l = l * corr + sum;
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) o[u] *= corr;
+      for (unsigned long long left = __ballot(sees); left != 0; left &= left - 1) {
+        const int j = __builtin_ctzll(left);
+        const float pj = __shfl(p, j);
+        const uint16_t* vj = (const uint16_t*)(uintptr_t)__shfl((unsigned long long)(uintptr_t)v, j);
+#pragma unroll
+        for (int u = 0; u < D / 64; ++u) o[u] = fmaf(pj, __uint_as_float((unsigned)vj[lane + 64 * u] << 16), o[u]);
+      }
+    }
+    bool finite = true;
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u) finite &= __builtin_isfinite(o[u]);
+    if (__ballot(!finite) == 0) continue;
+    if (whole) {
+      uint16_t* out = (uint16_t*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2];
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) out[lane + 64 * u] = __builtin_bit_cast(uint16_t, (__bf16)(o[u] / l));
+    } else {
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) a->ws_o[(slot0 + R) * D + lane + 64 * u] = o[u];
+      if (lane == 0) { a->ws_ml[2 * (slot0 + R)] = m; a->ws_ml[2 * (slot0 + R) + 1] = l; }
+    }
+  }
+}
 
 // Kernels by query rows per (sequence, K/V head): up to 32 (stream), more (tile); both bf16
 size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block);

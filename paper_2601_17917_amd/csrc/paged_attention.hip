@@ -103,7 +103,7 @@ hipError_t launch_paged_attention(const sdllm_paged_attn_params& p, const void* 
   dense_or(p.out_stride, p.Hq, p.K, p.D, a.o_st);
   dense_or(p.k_block_stride, p.Hkv, p.K, p.D, a.kb_st);
   dense_or(p.v_block_stride, p.Hkv, p.K, p.D, a.vb_st);
-  a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.R = a.g * p.K; a.shift = __builtin_ctz(p.page_size);
+  a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.R = a.g * p.K; a.shift = __builtin_ctz(p.page_size); a.page_bytes = (unsigned)((long long)p.Hkv * p.page_size * p.D * 2);
   a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.max_kv = p.max_kv_len; a.causal = p.causal; a.window = p.window; a.sinks = p.sinks;
   a.scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.D);
   a.scale_log2 = a.scale * kLog2e; a.thr8 = 8.0f / a.scale_log2;

@@ -19,85 +19,40 @@ namespace sdllm {
 template <int D> struct StreamShape {
   static constexpr int TK = 4096 / D;              // keys per tile
   static constexpr int KB = TK / 16;               // 16-key slabs
-  static constexpr int CPR = D / 8, RPI = 64 / CPR, IPT = 16 / RPI, R256 = 16 / CPR;
   static constexpr int NS = D / 32, NDB = D / 16, ROWB = D * 2;
   static constexpr int SLABB = 16 * ROWB, VB = TK * ROWB, WAVEB = 2 * VB;
 };
 
-// Where the keys of a tile come from.  `vis`: bit 16 s + r: row r of slab s holds a key that some query row sees (all others are
-// zero in LDS).  Per-lane constants of the transfers: byte offset of the lane's (swizzled) chunk of transfer j minus j KiB.
-template <int D> struct StreamLane {
-  unsigned kgj[4], vgj[4];
-  int rowj[4], kcj[4], vcj[4];                     // row within the slab and byte in the row, for slabs moved row by row
-  unsigned kro[StreamShape<D>::NS], vro[StreamShape<D>::NDB];
-  unsigned base;                                   // LDS address of the wave's area
-};
-
-// Page ids of a tile's slabs (entries past the table's end repeat the last one)
+// Puts tile u.i in flight.  Returns which of its keys some query row sees (bit r: key r; the rows of the others are zero).
 template <int D>
-__device__ __forceinline__ void load_pages(const PagedArgs& a, const Unit& u, int i, int (&ids)[StreamShape<D>::KB]) {
-  using S = StreamShape<D>;
-  const const_i32_ptr row = (const_i32_ptr)(uintptr_t)(a.table + (long long)u.b * a.max_pages);
-  const int k0 = u.s.tile(i) * S::TK;
-#pragma unroll
-  for (int j = 0; j < S::KB; ++j) ids[j] = row[min((k0 + 16 * j) >> a.shift, a.max_pages - 1)];
-}
-
-template <int D>
-__device__ __forceinline__ unsigned long long issue_tile(const PagedArgs& a, const StreamLane<D>& L, const Unit& u,
-                                                         const int (&ids)[StreamShape<D>::KB], unsigned char* lds_wave) {
+__device__ __forceinline__ unsigned long long issue_tile(const Hot& h, const Unit& u, Pages& pages, unsigned base,
+                                                         unsigned char* lds_wave) {
   using S = StreamShape<D>;
   const Seen& s = u.s;
-  const int lane = threadIdx.x & 63;
-  unsigned long long vis = 0;
   if (s.tiles == 0) return 0;                      // nothing to see, nothing is read from LDS either
   const int k0 = s.tile(u.i) * S::TK;
+  pages.seek(h, k0);
+  constexpr unsigned long long kAll = S::TK == 64 ? ~0ull : (1ull << S::TK) - 1;
+  const bool plain = pages.all_ok<S::TK>(h, k0) && ((k0 >= s.lo && k0 + S::TK - 16 <= s.last16) || k0 + S::TK - 16 <= s.sink16);
+  const unsigned long long vis = plain ? kAll : seen_keys<S::TK>(h, s, pages, k0);
 #pragma unroll
   for (int j = 0; j < S::KB; ++j) {
     const int k = k0 + 16 * j;
-    const bool valid = (unsigned)ids[j] < (unsigned)a.n_pages;
-    const long long row0 = (((long long)ids[j] * a.Hkv + u.kvh) << a.shift) + (k & ((1 << a.shift) - 1));
-    if (valid && k + 16 <= s.n && ((k >= s.lo && k + 16 <= s.hi) || k + 16 <= s.sink)) {
-      dma_slab<S::IPT, true>(L.base + j * S::SLABB, uniform_ptr((const unsigned char*)a.kp + row0 * S::ROWB), L.kgj);
-      dma_slab<S::IPT, true>(L.base + S::VB + j * S::SLABB, uniform_ptr((const unsigned char*)a.vp + row0 * S::ROWB), L.vgj);
-      vis |= 0xffffull << (16 * j);
-      continue;
-    }
-    // a border of what is seen, the end of the cache, rows of the block, a page that is not there: row by row, and zeros
-    // where there is no key
-    const int key = k + (lane & 15);
-    const bool seen = key < s.hi && (key >= s.lo || key < s.sink) && (key >= s.n || valid);
-    const unsigned bits = (unsigned)__ballot(seen) & 0xffffu;
-    vis |= (unsigned long long)bits << (16 * j);
-#pragma unroll
-    for (int t = 0; t < S::IPT; ++t) {
-      *reinterpret_cast<u32x4*>(lds_wave + j * S::SLABB + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
-      *reinterpret_cast<u32x4*>(lds_wave + S::VB + j * S::SLABB + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
-    }
-    wait_lds();
-#pragma unroll
-    for (int t = 0; t < S::IPT; ++t) {
-      const int r = L.rowj[t];
-      if ((bits >> r) & 1) {
-        const unsigned char *kr, *vr;
-        if (k + r < s.n) {
-          kr = (const unsigned char*)a.kp + (row0 + r) * S::ROWB;
-          vr = (const unsigned char*)a.vp + (row0 + r) * S::ROWB;
-        } else {
-          const long long x = k + r - s.n;
-          kr = (const unsigned char*)a.kb + 2 * (u.b * a.kb_st[0] + u.kvh * a.kb_st[1] + x * a.kb_st[2]);
-          vr = (const unsigned char*)a.vb + 2 * (u.b * a.vb_st[0] + u.kvh * a.vb_st[1] + x * a.vb_st[2]);
-        }
-        dma16_vaddr<true>(L.base + j * S::SLABB + 1024 * t, kr + L.kcj[t]);
-        dma16_vaddr<true>(L.base + S::VB + j * S::SLABB + 1024 * t, vr + L.vcj[t]);
-      }
+    const unsigned bits = (unsigned)(vis >> (16 * j)) & 0xffffu;
+    const unsigned long long at = row_offset(h, pages.of(h, k), u.kvh, k, S::ROWB);
+    if (bits == 0xffffu && k + 16 <= s.n) {
+      move_slab<D, true, false>(base + j * S::SLABB, h.kp + at);
+      move_slab<D, true, true>(base + S::VB + j * S::SLABB, h.vp + at);
+    } else {
+      move_rows<D, true, false>(s, u.b, u.kvh, k, bits, h.kp + at, base + j * S::SLABB, lds_wave + j * S::SLABB);
+      move_rows<D, true, true>(s, u.b, u.kvh, k, bits, h.vp + at, base + S::VB + j * S::SLABB, lds_wave + S::VB + j * S::SLABB);
     }
   }
   return vis;
 }
 
 template <int D, int RB>
-__global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
   using S = StreamShape<D>;
   constexpr int TK = S::TK, KB = S::KB, NS = S::NS, NDB = S::NDB, U = TK / 32;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * S::WAVEB];
@@ -107,65 +62,51 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
 
   // this wave's tiles
   const int worker = blockIdx.x * 4 + wave;
-  if (worker >= a.workers) return;
   Unit nxt;
-  long long f, f1;
-  if (a.min_tiles == 0) {                          // a wave per (sequence, K/V head)
-    open_unit<TK>(a, nxt, worker / a.Hkv, worker % a.Hkv, 0);
-    f = 0; f1 = nxt.T;
-    if (f1 == 0) return;
-  } else {
-    const long long total = all_tiles<TK>(a), per = tiles_per_worker(a, total);
-    f = worker * per; f1 = f + per < total ? f + per : total;
-    if (f >= f1) return;
-    locate<TK>(a, f, nxt);
-  }
-  int ids[KB];
-  load_pages<D>(a, nxt, nxt.i, ids);
-
-  StreamLane<D> L;
-  L.base = uniform((int)(unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_wave);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int jj = j < S::IPT ? j : 0, r = S::RPI * jj + lane / S::CPR, c = lane % S::CPR;
-    L.rowj[j] = r;
-    L.kcj[j] = (c ^ ((r / S::R256) % S::CPR)) << 4;
-    L.vcj[j] = (c ^ (2 * ((r / S::R256) % (S::CPR / 2)))) << 4;
-    L.kgj[j] = r * S::ROWB + L.kcj[j] - 1024 * jj;
-    L.vgj[j] = r * S::ROWB + L.vcj[j] - 1024 * jj;
-  }
+  int left;                                        // tiles of its share still to do
   {
-    const int fk = (D == 128) ? l16 : (l16 >> 1);
-#pragma unroll
-    for (int s2 = 0; s2 < NS; ++s2) L.kro[s2] = l16 * S::ROWB + (((4 * s2 + G) ^ fk) << 4);
-    const int e4 = l16 >> 2, c4 = l16 & 3;
-    const int fv = (D == 128) ? 2 * (4 * (G & 1) + e4) : 2 * (2 * (G & 1) + (e4 >> 1));
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-      L.vro[db] = S::VB + (4 * G + e4) * S::ROWB + (((2 * db + (c4 >> 1)) ^ fv) << 4) + ((c4 & 1) << 3);
+    const Args a = arguments();
+    if (worker >= a->workers) return;
+    if (a->min_tiles == 0) {                       // a wave per (sequence, K/V head)
+      open_unit<TK>(nxt, worker / a->Hkv, worker % a->Hkv, 0);
+      left = nxt.T;
+    } else {
+      left = open_share<TK>(worker, nxt);
+    }
   }
-  unsigned long long vis_next = issue_tile<D>(a, L, nxt, ids, lds_wave);
-  load_pages<D>(a, nxt, min(nxt.i + 1, nxt.T - 1), ids);
+  if (left == 0) return;
+  const Hot h = hot_arguments();
+  Pages pages;
+  pages.open(nxt.b);
+  const unsigned base = uniform((int)(unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_wave);
+  unsigned long long vis_next = issue_tile<D>(h, nxt, pages, base, lds_wave);
+  // LDS offsets of the lane's operands of slice 0 / d block 0; the others flip bits of them
+  const unsigned kro = l16 * S::ROWB + ((G ^ ((D == 128) ? l16 : (l16 >> 1))) << 4);
+  const int e4 = l16 >> 2, c4 = l16 & 3, fv = (D == 128) ? 2 * (4 * (G & 1) + e4) : 2 * (2 * (G & 1) + (e4 >> 1));
+  const unsigned vro = S::VB + (4 * G + e4) * S::ROWB + (((c4 >> 1) ^ fv) << 4) + ((c4 & 1) << 3);
 
   int part = 0;                                    // of this wave: the first unit's partial result goes to slot 0, the last's to 1
-  while (f < f1) {
+  while (left > 0) {
     // ---- a unit: its query rows as MFMA B operands (lane: row l16, d = 32 s + 8 G .. + 7)
     const Unit cur = nxt;
     const int begin = cur.i;
-    const int last_row = cur.s.q_len * a.g - 1;
     bf16x8 qreg[RB][NS];
-    int lo[RB], hi[RB];
+    int lo[RB], hi[RB], all_hi, all_lo;            // keys that row l16 sees, that all rows see
+    {
+      const Args a = arguments();
+      const int g = a->g, last_row = cur.s.q_len * g - 1;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int R = min(16 * rb + l16, last_row), r = R / a.g, h = cur.kvh * a.g + R - r * a.g;
-      const uint16_t* qp = (const uint16_t*)a.q + cur.b * a.q_st[0] + h * a.q_st[1] + r * a.q_st[2];
+      for (int rb = 0; rb < RB; ++rb) {
+        const int R = min(16 * rb + l16, last_row), r = R / g, hq = cur.kvh * g + R - r * g;
+        const uint16_t* qp = (const uint16_t*)a->q + cur.b * a->q_st[0] + hq * a->q_st[1] + r * a->q_st[2];
 #pragma unroll
-      for (int s2 = 0; s2 < NS; ++s2) qreg[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
-      row_range(a, cur.s, r, lo[rb], hi[rb]);
+        for (int s2 = 0; s2 < NS; ++s2) qreg[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
+        row_range(a, cur.s, r, lo[rb], hi[rb]);
+      }
+      int x;
+      row_range(a, cur.s, 0, x, all_hi);
+      row_range(a, cur.s, max(cur.s.q_len - 1, 0), all_lo, x);
     }
-    // keys that all rows see: up to all_hi, from all_lo on
-    const int all_hi = a.causal ? min(max(cur.s.p0 + 1, 0), cur.s.N) : cur.s.N;
-    const int all_lo = a.window > 0 ? max(cur.s.p1 - a.window + 1, 0) : 0;
     f32x4 o[RB][NDB];
     f32x4 neg_m[RB];                               // minus the reference of row l16, in score units, four times
     float thr[RB], lsum[RB];                       // kNegBig: no reference yet
@@ -175,8 +116,9 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
 #pragma unroll
       for (int db = 0; db < NDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    bool redo = false;
     int i = begin;
-    for (; i < cur.T && f < f1; ++i, ++f) {
+    for (; i < cur.T && left > 0; ++i, --left) {
       const unsigned long long vis = vis_next;
       wait_transfers();
       bf16x8 kop[KB][NS];
@@ -185,23 +127,22 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *reinterpret_cast<const bf16x8*>(lds_wave + L.kro[s2] + kb * S::SLABB);
+          for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *reinterpret_cast<const bf16x8*>(lds_wave + (kro ^ (s2 << 6)) + kb * S::SLABB);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int db = 0; db < NDB; ++db) {
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds_wave + L.vro[db] + 32 * u * S::ROWB));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds_wave + L.vro[db] + (32 * u + 16) * S::ROWB));
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds_wave + (vro ^ (db << 5)) + 32 * u * S::ROWB));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds_wave + (vro ^ (db << 5)) + (32 * u + 16) * S::ROWB));
             vop[u][db] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
           }
       }
       // the operands are in registers: the area takes the next tile
       wait_lds();
-      if (f + 1 < f1) {
-        next_tile<TK>(a, nxt);
-        if (nxt.i == 0) load_pages<D>(a, nxt, nxt.i, ids);       // a unit's first tile; the others' ids came in ahead
-        vis_next = issue_tile<D>(a, L, nxt, ids, lds_wave);
-        load_pages<D>(a, nxt, min(nxt.i + 1, nxt.T - 1), ids);
+      if (left > 1) {
+        next_tile<TK>(nxt);
+        if (nxt.b != cur.b) pages.open(nxt.b);
+        vis_next = issue_tile<D>(h, nxt, pages, base, lds_wave);
       }
       if (vis == 0) continue;
 
@@ -220,19 +161,11 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
             sacc[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[kb][s2], qreg[rb][s2], sacc[rb][kb], 0, 0, 0);
       const int k0 = cur.s.tile(i) * TK;
       constexpr unsigned long long kAll = KB == 4 ? ~0ull : (1ull << (16 * KB)) - 1;
-      const bool masked = vis != kAll || k0 + TK > all_hi || (k0 < all_lo && k0 + TK > a.sinks);
+      const bool missing = vis != kAll, above = k0 + TK > all_hi, below = k0 < all_lo && k0 + TK > h.sinks;
+      const bool masked = missing || above || below;
       if (masked) {
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int key = k0 + 16 * kb + 4 * G + e;
-              // (without short circuits: those are branches here)
-              const bool see = (((unsigned)(vis >> (16 * kb)) >> (4 * G + e)) & 1) & (key < hi[rb]) & ((key >= lo[rb]) | (key < a.sinks));
-              sacc[rb][kb][e] = see ? sacc[rb][kb][e] : -INFINITY;
-            }
+        for (int rb = 0; rb < RB; ++rb) hide<KB>(sacc[rb], k0, lo[rb], hi[rb], h.sinks, vis, missing, above, below);
       }
       // ---- online softmax: p = exp2((s - reference) scale_log2)
       s16x8 pk[RB][U];
@@ -249,19 +182,19 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
           mx = fmaxf(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
           const bool move = mx > thr[rb];
           const float shift = move ? mx : 0.f;
-          const float corr = thr[rb] == kNegBig ? 0.f : exp2_fast(-shift * a.scale_log2);
+          const float corr = thr[rb] == kNegBig ? 0.f : exp2_fast(-shift * h.scale_log2);
           lsum[rb] *= corr;
 #pragma unroll
           for (int db = 0; db < NDB; ++db) o[rb][db] *= corr;
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) sacc[rb][kb] -= shift;
           neg_m[rb] -= shift;
-          thr[rb] = move ? a.thr8 : thr[rb];
+          thr[rb] = move ? h.thr8 : thr[rb];
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sacc[rb][kb][e] = exp2_fast(sacc[rb][kb][e] * a.scale_log2);
+          for (int e = 0; e < 4; ++e) sacc[rb][kb][e] = exp2_fast(sacc[rb][kb][e] * h.scale_log2);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           union { uint32_t w[4]; s16x8 v; } cv;
@@ -281,26 +214,13 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
         lsum[rb] = ls[0];
       }
       if (masked && cur.s.p1 > cur.s.p0) {         // rows at different positions: what a row does not see must not reach it
-        bool bad = false;
+        unsigned bad = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int db = 0; db < NDB; ++db) bad |= has_nonfinite(__builtin_bit_cast(u32x4, vop[u][db]));
-        if (__builtin_expect(__ballot(bad) != 0, 0)) {
-#pragma unroll 1
-          for (int kind = 0; kind < 3; ++kind)
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb) {
-                f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is_kind(vop[u][db], kind)),
-                                                              __builtin_bit_cast(bf16x8, weighed(pk[rb][u])), c, 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[rb][db][e] += c[e] != 0.f ? of_kind(kind) : 0.f;
-              }
+          for (int db = 0; db < NDB; ++db) bad |= nonfinite_bits(__builtin_bit_cast(u32x4, vop[u][db]));
+        if (__builtin_expect(__ballot(bad != 0) != 0, 0)) {
+          redo = true;
 #pragma unroll
           for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -319,15 +239,18 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
     }
 
     // ---- this wave's share of the unit is done
+    const Args a = arguments();
     const bool whole = begin == 0 && i == cur.T;
+    const int g = a->g, last_row = cur.s.q_len * g - 1;
+    const long long slot0 = ((long long)worker * 2 + part) * a->R;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int R = 16 * rb + l16;
       if (R > last_row) continue;
       if (whole) {
         const float inv = lsum[rb] == 0.f ? 0.f : 1.0f / lsum[rb];
-        const int r = R / a.g, h = cur.kvh * a.g + R - r * a.g;
-        uint16_t* orow = (uint16_t*)a.out + cur.b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2];
+        const int r = R / g, hq = cur.kvh * g + R - r * g;
+        uint16_t* orow = (uint16_t*)a->out + cur.b * a->o_st[0] + hq * a->o_st[1] + r * a->o_st[2];
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
           uint2 w;
@@ -336,12 +259,12 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
           *reinterpret_cast<uint2*>(orow + 16 * db + 4 * G) = w;
         }
       } else {
-        const long long slot = ((long long)worker * 2 + part) * a.R + R;
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(a.ws_o + slot * D + 16 * db + 4 * G) = o[rb][db];
-        if (G == 0) { a.ws_ml[2 * slot] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; a.ws_ml[2 * slot + 1] = lsum[rb]; }
+        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(a->ws_o + (slot0 + R) * D + 16 * db + 4 * G) = o[rb][db];
+        if (G == 0) { a->ws_ml[2 * (slot0 + R)] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; a->ws_ml[2 * (slot0 + R) + 1] = lsum[rb]; }
       }
     }
+    if (redo) redo_rows<D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, slot0);
     part = 1;
   }
 }
@@ -349,27 +272,28 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs a) {
 // Merges the shares of every output row that several workers (waves here, workgroups of the tile kernel) walked, in the order of the tiles.  A workgroup per row: 256 / (D / 4)
 // groups of lanes take every so many-th share, then one adds up the groups, in order.
 template <int D, int TK>
-__global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
+  const Args a = arguments();
   constexpr int TPR = D / 4, NG = 256 / TPR;
   __shared__ f32x4 o_s[NG][TPR];
   __shared__ float m_s[NG], l_s[NG];
-  const unsigned unit = blockIdx.x / (unsigned)a.R;
-  const int R = blockIdx.x - unit * a.R, b = unit / (unsigned)a.Hkv, kvh = unit - b * a.Hkv;
+  const unsigned unit = blockIdx.x / (unsigned)a->R;
+  const int R = blockIdx.x - unit * a->R, b = unit / (unsigned)a->Hkv, kvh = unit - b * a->Hkv;
   // where the unit's tiles lie among the call's
   const int lane = threadIdx.x & 63;
   long long total = 0, start = 0;
   int T = 0, q_len = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
+  for (int b0 = 0; b0 < a->B; b0 += 64) {
     const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
     if (b >= b0 && b < b0 + 64) {
       T = uniform(__shfl(t, b - b0));
-      start = (total + uniform(__shfl(upto, b - b0)) - T) * a.Hkv + (long long)kvh * T;
+      start = (total + uniform(__shfl(upto, b - b0)) - T) * a->Hkv + (long long)kvh * T;
     }
     total += uniform(__shfl(upto, 63));
   }
-  total *= a.Hkv;
-  q_len = min(max(a.q_lens ? a.q_lens[b] : a.K, 0), a.K);
-  if (T == 0 || R >= q_len * a.g) return;
+  total *= a->Hkv;
+  q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
+  if (T == 0 || R >= q_len * a->g) return;
   const long long per = tiles_per_worker(a, total);
   const int w0 = (int)(start / per), w1 = (int)((start + T - 1) / per);
   if (w0 == w1) return;                            // written by its wave
@@ -378,10 +302,10 @@ __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs a) {
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int w = w0 + grp; w <= w1; w += NG) {
     // the unit is its wave's first one unless the wave began before it
-    const long long slot = ((long long)w * 2 + (start > w * per ? 1 : 0)) * a.R + R;
-    const f32x4 ov = *reinterpret_cast<const f32x4*>(a.ws_o + slot * D + d);
-    const float mk = a.ws_ml[2 * slot], lk = a.ws_ml[2 * slot + 1];
-    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a.scale_log2), c1 = exp2_fast((mk - up) * a.scale_log2);
+    const long long slot = ((long long)w * 2 + (start > w * per ? 1 : 0)) * a->R + R;
+    const f32x4 ov = *reinterpret_cast<const f32x4*>(a->ws_o + slot * D + d);
+    const float mk = a->ws_ml[2 * slot], lk = a->ws_ml[2 * slot + 1];
+    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
     acc = acc * c0 + ov * c1;
     l = l * c0 + lk * c1;
     M = up;
@@ -392,17 +316,17 @@ __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs a) {
   if (grp != 0) return;
 #pragma unroll
   for (int k = 1; k < NG; ++k) {
-    const float up = fmaxf(M, m_s[k]), c0 = exp2_fast((M - up) * a.scale_log2), c1 = exp2_fast((m_s[k] - up) * a.scale_log2);
+    const float up = fmaxf(M, m_s[k]), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((m_s[k] - up) * a->scale_log2);
     acc = acc * c0 + o_s[k][threadIdx.x % TPR] * c1;
     l = l * c0 + l_s[k] * c1;
     M = up;
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int r = R / a.g, h = kvh * a.g + R - r * a.g;
+  const int r = R / a->g, h = kvh * a->g + R - r * a->g;
   uint2 w2;
   w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
   w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-  *reinterpret_cast<uint2*>((uint16_t*)a.out + b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2] + d) = w2;
+  *reinterpret_cast<uint2*>((uint16_t*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2] + d) = w2;
 }
 
 // ---- launch plan, from the parameters alone

@@ -2,8 +2,8 @@
 // rows of a block over its heads, the pieces of prompts.
 //
 // A workgroup owns 16 RB NW query rows (NW waves, 16 RB rows each) and walks key tiles of 64 that its waves share through a
-// two-stage ring in LDS: each wave moves 16-row slabs global -> LDS, one tile ahead of the one being computed, one barrier per
-// tile.  Products, operand layouts and the softmax are those of the stream kernel.
+// ring in LDS: each wave moves 16-row slabs global -> LDS, one tile ahead of the one being computed (four waves, two workgroups per CU)
+// or two (eight waves, one workgroup per CU), one barrier per tile.  Products, operand layouts and the softmax are those of the stream kernel.
 //   FLAT: one row tile covers a (sequence, K/V head).  The workgroups walk equal shares of all key tiles of the call, laid end to end
 //         as the stream kernel's waves do, so that lengths need not be alike.
 //   else: a workgroup per (row tile, sequence, K/V head, part of the keys it sees); the tiles of the last rows, which see most under a
@@ -13,99 +13,35 @@
 namespace sdllm {
 
 constexpr int kTK = 64;                            // keys per tile
+typedef const bf16x8 __attribute__((address_space(3))) * lds_bf16x8_ptr;
+typedef u32x4 __attribute__((address_space(3))) * lds_u32x4_ptr;
+typedef int __attribute__((address_space(3))) * lds_int_ptr;
 
 template <int D, int NST> struct TileShape {
-  static constexpr int CPR = D / 8, RPI = 64 / CPR, IPT = 16 / RPI, R256 = 16 / CPR;
   static constexpr int NS = D / 32, NDB = D / 16, ROWB = D * 2;
-  static constexpr int SLABB = 16 * ROWB, STAGEB = kTK * ROWB, VB = NST * STAGEB, LDS = 2 * NST * STAGEB + NST * 16;
+  static constexpr int SLABB = 16 * ROWB, STAGEB = kTK * ROWB, VB = NST * STAGEB, FLAG = 2 * NST * STAGEB, LDS = FLAG + 16;
 };
-
-// Moves the 16-row slab `slab` of the tile at key k0 into LDS: K (kind 0), V (kind 1) or both.  Returns which of its rows hold a key that
-// some query row of the tile sees; the others are zero.
-template <int D, int NST, bool ONCE, int KINDS>
-__device__ __forceinline__ unsigned move_slab(const PagedArgs& a, const Unit& u, int k, int id, int kind, unsigned lds_slab,
-                                              unsigned char* slab_ptr, unsigned kg, unsigned vg) {
-  using S = TileShape<D, NST>;
-  // byte offset of the lane's (swizzled) 16 bytes of transfer j within the slab, less j KiB; made where they are used, of two
-  // registers that the compiler cannot see through: kept over the loop they cost eight
-  asm volatile("" : "+v"(kg), "+v"(vg));
-  const unsigned kgj[4] = {kg, kg ^ 64, kg ^ 128, kg ^ 192};
-  const unsigned vodd = D == 128 ? vg ^ 128 : vg;
-  const unsigned vgj[4] = {vg, vodd, vg, vodd};
-  const Seen& s = u.s;
-  const int lane = threadIdx.x & 63;
-  const bool valid = (unsigned)id < (unsigned)a.n_pages;
-  const long long row0 = (((long long)id * a.Hkv + u.kvh) << a.shift) + (k & ((1 << a.shift) - 1));
-  if (valid && k + 16 <= s.n && ((k >= s.lo && k + 16 <= s.hi) || k + 16 <= s.sink)) {
-    if (KINDS == 2 || kind == 0) dma_slab<S::IPT, ONCE>(lds_slab, uniform_ptr((const unsigned char*)a.kp + row0 * S::ROWB), kgj);
-    if (KINDS == 2 || kind == 1) dma_slab<S::IPT, ONCE>(lds_slab + S::VB, uniform_ptr((const unsigned char*)a.vp + row0 * S::ROWB), vgj);
-    return 0xffffu;
-  }
-  // 16 rows of the block, all of them seen
-  if (k >= s.n && k >= s.lo && k + 16 <= s.hi && a.kb_st[2] == D && a.vb_st[2] == D) {
-    const long long x = k - s.n;
-    if (KINDS == 2 || kind == 0)
-      dma_slab<S::IPT, ONCE>(lds_slab, uniform_ptr((const unsigned char*)a.kb + 2 * (u.b * a.kb_st[0] + u.kvh * a.kb_st[1] + x * D)), kgj);
-    if (KINDS == 2 || kind == 1)
-      dma_slab<S::IPT, ONCE>(lds_slab + S::VB, uniform_ptr((const unsigned char*)a.vb + 2 * (u.b * a.vb_st[0] + u.kvh * a.vb_st[1] + x * D)), vgj);
-    return 0xffffu;
-  }
-  // a border of what is seen, the end of the cache, a page that is not there: row by row, and zeros where there is no key
-  const int key = k + (lane & 15);
-  const bool seen = (key < s.hi) & ((key >= s.lo) | (key < s.sink)) & ((key >= s.n) | valid);
-  const unsigned bits = (unsigned)__ballot(seen) & 0xffffu;
-#pragma unroll
-  for (int t = 0; t < S::IPT; ++t) {
-    if (KINDS == 2 || kind == 0) *reinterpret_cast<u32x4*>(slab_ptr + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
-    if (KINDS == 2 || kind == 1) *reinterpret_cast<u32x4*>(slab_ptr + S::VB + 1024 * t + 16 * lane) = u32x4{0, 0, 0, 0};
-  }
-  wait_lds();
-#pragma unroll
-  for (int t = 0; t < S::IPT; ++t) {
-    const int r = S::RPI * t + lane / S::CPR;
-    if ((bits >> r) & 1) {
-      // kgj holds row, chunk and minus t KiB; the row is taken off again: it may lie elsewhere
-      const int kc = kgj[t] + 1024 * t - r * S::ROWB, vc = vgj[t] + 1024 * t - r * S::ROWB;
-      const unsigned char *kr, *vr;
-      if (k + r < s.n) {
-        kr = (const unsigned char*)a.kp + (row0 + r) * S::ROWB;
-        vr = (const unsigned char*)a.vp + (row0 + r) * S::ROWB;
-      } else {
-        const long long x = k + r - s.n;
-        kr = (const unsigned char*)a.kb + 2 * (u.b * a.kb_st[0] + u.kvh * a.kb_st[1] + x * a.kb_st[2]);
-        vr = (const unsigned char*)a.vb + 2 * (u.b * a.vb_st[0] + u.kvh * a.vb_st[1] + x * a.vb_st[2]);
-      }
-      if (KINDS == 2 || kind == 0) dma16_vaddr<ONCE>(lds_slab + 1024 * t, kr + kc);
-      if (KINDS == 2 || kind == 1) dma16_vaddr<ONCE>(lds_slab + S::VB + 1024 * t, vr + vc);
-    }
-  }
-  return bits;
-}
-
-__device__ __forceinline__ int page_id(const PagedArgs& a, const Unit& u, int k) {
-  const const_i32_ptr row = (const_i32_ptr)(uintptr_t)(a.table + (long long)u.b * a.max_pages);
-  return row[min(k >> a.shift, a.max_pages - 1)];
-}
 
 // What a wave keeps over the tiles of a unit
 template <int D, int RB> struct Rows {
   static constexpr int NS = D / 32, NDB = D / 16;
   bf16x8 q[RB][NS];                                // MFMA B operands (lane: row l16, d = 32 s + 8 G .. + 7)
   f32x4 o[RB][NDB];
-  f32x4 neg_m[RB];                                 // minus the reference of row l16, four times
+  float neg_m[RB];                                 // minus the reference of row l16
   float thr[RB], lsum[RB];                         // thr kNegBig: no reference yet; lsum: RB == 1 the row's, else this lane's part
-  int lo[RB], hi[RB];                              // keys that row l16 sees
+  int pos[RB];                                     // position of row l16
 };
 
-// One key tile; kro, vro: LDS offsets of the lane's first operands in the tile's ring stage
+// One key tile.  kro, vro: LDS addresses of the lane's first operands in the tile's ring stage
 template <int D, int RB, int NST>
-__device__ __forceinline__ void compute_tile(const PagedArgs& a, Rows<D, RB>& w, const unsigned char* lds, unsigned kro, unsigned vro, unsigned vtile, int k0, bool masked, bool rows_differ, u32x4 vbits) {
+__device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsigned kro, unsigned vro, int k0, bool missing, bool above,
+                                             bool below, unsigned long long vis) {
   using S = TileShape<D, NST>;
   constexpr int NS = S::NS, NDB = S::NDB;
-  const int G = (threadIdx.x & 63) >> 4;
+  __builtin_amdgcn_iglp_opt(0);                    // the compiler's interleaving of matrix instructions and LDS reads
   auto read_vt = [&](int db, int u) {
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds + (vro ^ (db << 5)) + 32 * u * S::ROWB));
-    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds + (vro ^ (db << 5)) + (32 * u + 16) * S::ROWB));
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)((vro ^ (db << 5)) + 32 * u * S::ROWB));
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)((vro ^ (db << 5)) + (32 * u + 16) * S::ROWB));
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
   };
   // ---- S^T = K Q^T - reference
@@ -113,26 +49,18 @@ __device__ __forceinline__ void compute_tile(const PagedArgs& a, Rows<D, RB>& w,
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) sacc[rb][kb] = w.neg_m[rb];
+    for (int kb = 0; kb < 4; ++kb) sacc[rb][kb] = f32x4{w.neg_m[rb], w.neg_m[rb], w.neg_m[rb], w.neg_m[rb]};
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
     for (int s2 = 0; s2 < NS; ++s2) {
-      const bf16x8 kop = *reinterpret_cast<const bf16x8*>(lds + (kro ^ (s2 << 6)) + kb * S::SLABB);
+      const bf16x8 kop = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) sacc[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, w.q[rb][s2], sacc[rb][kb], 0, 0, 0);
     }
-  if (masked) {
+  if (missing || above || below) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = k0 + 16 * kb + 4 * G + e;
-          const bool see = ((vbits[kb] >> (4 * G + e)) & 1) & (key < w.hi[rb]) & ((key >= w.lo[rb]) | (key < a.sinks));
-          sacc[rb][kb][e] = see ? sacc[rb][kb][e] : -INFINITY;
-        }
+    for (int rb = 0; rb < RB; ++rb) hide<4>(sacc[rb], k0, w.pos[rb] - h.window + 1, w.pos[rb] + 1, h.sinks, vis, missing, above, below);
   }
   // ---- online softmax
   s16x8 pk[RB][2];
@@ -153,21 +81,21 @@ __device__ __forceinline__ void compute_tile(const PagedArgs& a, Rows<D, RB>& w,
       mx = fmaxf(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
       const bool move = mx > w.thr[rb];
       const float shift = move ? mx : 0.f;
-      const float corr = w.thr[rb] == kNegBig ? 0.f : exp2_fast(-shift * a.scale_log2);
+      const float corr = w.thr[rb] == kNegBig ? 0.f : exp2_fast(-shift * h.scale_log2);
       w.lsum[rb] *= corr;
 #pragma unroll
       for (int db = 0; db < NDB; ++db) w.o[rb][db] *= corr;
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) sacc[rb][kb] -= shift;
       w.neg_m[rb] -= shift;
-      w.thr[rb] = move ? a.thr8 : w.thr[rb];
+      w.thr[rb] = move ? h.thr8 : w.thr[rb];
     }
     float ps = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p = exp2_fast(sacc[rb][kb][e] * a.scale_log2);
+        const float p = exp2_fast(sacc[rb][kb][e] * h.scale_log2);
         sacc[rb][kb][e] = p;
         if (RB != 1) ps += p;
       }
@@ -192,40 +120,6 @@ __device__ __forceinline__ void compute_tile(const PagedArgs& a, Rows<D, RB>& w,
     w.lsum[0] = ls[0];
   }
   // ---- O^T += V^T P^T
-  if (masked && rows_differ) {                     // what a row does not see must not reach it
-    const int lane = threadIdx.x & 63;
-    bool bad = false;
-#pragma unroll 4
-    for (int it = 0; it < S::STAGEB / 1024; ++it) bad |= has_nonfinite(*reinterpret_cast<const u32x4*>(lds + vtile + 1024 * it + 16 * lane));
-    if (__builtin_expect(__ballot(bad) != 0, 0)) {
-#pragma unroll 1
-      for (int kind = 0; kind < 3; ++kind)
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          asm volatile("" ::: "memory");           // keeps the reads where they are: all of them at once do not fit the registers
-          const s16x8 v0 = is_kind(read_vt(db, 0), kind), v1 = is_kind(read_vt(db, 1), kind);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) {
-            f32x4 c = {0.f, 0.f, 0.f, 0.f};
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v0), __builtin_bit_cast(bf16x8, weighed(pk[rb][0])), c, 0, 0, 0);
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v1), __builtin_bit_cast(bf16x8, weighed(pk[rb][1])), c, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w.o[rb][db][e] += c[e] != 0.f ? of_kind(kind) : 0.f;
-          }
-        }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          asm volatile("" ::: "memory");
-          const s16x8 vop = finite_part(read_vt(db, u));
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-            w.o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop), __builtin_bit_cast(bf16x8, pk[rb][u]), w.o[rb][db], 0, 0, 0);
-        }
-      return;
-    }
-  }
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -238,126 +132,205 @@ __device__ __forceinline__ void compute_tile(const PagedArgs& a, Rows<D, RB>& w,
 }
 
 template <int D, int RB, int NW, bool FLAT>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(PagedArgs a) {
-  constexpr int NST = 2, WROWS = 16 * RB, KINDS = NW == 8 ? 1 : 2;
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(PagedArgs) {
+  constexpr int NST = NW == 8 ? 3 : 2, WROWS = 16 * RB;
   constexpr bool ONCE = FLAT;                      // K/V is read by one workgroup only
   using S = TileShape<D, NST>;
-  constexpr int CPR = S::CPR, R256 = S::R256, NS = S::NS, NDB = S::NDB, ROWB = S::ROWB;
+  constexpr int NS = S::NS, NDB = S::NDB, ROWB = S::ROWB;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-  u32x4* vis_s = reinterpret_cast<u32x4*>(lds + 2 * NST * S::STAGEB);      // per stage: rows of the four slabs that hold a key
   const int lane = threadIdx.x & 63, l16 = lane & 15, G = lane >> 4;
-  const int wave = uniform(threadIdx.x >> 6), slab = wave & 3, kind = wave >> 2;
+  const int wave = uniform(threadIdx.x >> 6);
+  const int slab = wave & 3, kind = wave >> 2;     // four waves move K and V of a slab each, eight one of the two
 
   // ---- this workgroup's tiles
   Unit nxt;
-  long long f, f1, slot_unit = 0;
-  int row_base = 0;
-  if constexpr (FLAT) {
-    if (a.min_tiles == 0) {                        // a workgroup per (sequence, K/V head)
-      open_unit<kTK>(a, nxt, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, 0);
-      f = 0; f1 = nxt.T;
-    } else {
-      const long long total = all_tiles<kTK>(a), per = tiles_per_worker(a, total);
-      f = blockIdx.x * per; f1 = f + per < total ? f + per : total;
-      if (f >= f1) return;
-      locate<kTK>(a, f, nxt);
-    }
-  } else {
-    const unsigned units = (unsigned)(a.B * a.Hkv * a.parts);
-    const int rank = blockIdx.x / units, unit = blockIdx.x - rank * units;
-    const int part = unit % a.parts, bh = unit / a.parts;
-    nxt.b = bh / a.Hkv; nxt.kvh = bh - nxt.b * a.Hkv;
-    row_base = (a.row_tiles - 1 - rank) * (WROWS * NW);
-    const int r0 = row_base / a.g, r1 = (row_base + WROWS * NW - 1) / a.g;
-    nxt.s = seen_by(a, a.lens[nxt.b], a.q_lens ? a.q_lens[nxt.b] : a.K, r0, r1, kTK);
-    nxt.T = row_base < nxt.s.q_len * a.g ? max(nxt.s.tiles, 1) : 0;
-    const int per = max((nxt.T + a.parts - 1) / a.parts, a.min_tiles);
-    nxt.i = part * per;
-    f = nxt.i; f1 = min(nxt.i + per, nxt.T);
-    slot_unit = (long long)bh * a.parts + part;
-  }
-  if (f >= f1) return;
-
-  // LDS and source offsets of a lane; the others differ in bits that a slice, a block, a transfer number flips
-  const int row = lane / CPR, chunk = lane % CPR;
-  const unsigned kg = row * ROWB + ((chunk ^ ((row / R256) % CPR)) << 4), vg = row * ROWB + ((chunk ^ (2 * ((row / R256) % (CPR / 2)))) << 4);
-  unsigned kro, vro;                               // operands of slice 0 / d block 0 in the current ring stage
+  int left, row_base = 0;                          // tiles still to do; first query row
+  long long slot = 2LL * blockIdx.x;               // of its partial results
   {
-    kro = l16 * ROWB + ((G ^ ((D == 128) ? l16 : (l16 >> 1))) << 4);
-    const int e4 = l16 >> 2, c4 = l16 & 3;
-    const int fv = (D == 128) ? 2 * (4 * (G & 1) + e4) : 2 * (2 * (G & 1) + (e4 >> 1));
-    vro = S::VB + (4 * G + e4) * ROWB + (((c4 >> 1) ^ fv) << 4) + ((c4 & 1) << 3);
-  }
-  const unsigned lds_slab = uniform((int)(unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds) + slab * S::SLABB;
-
-  // tile of the unit at nxt into ring stage `stage`; `id`: the page of the wave's slab, the next tile's on return
-  auto issue = [&](int stage, int& id) {
-    unsigned bits = 0;
-    if (nxt.s.tiles > 0)
-      bits = move_slab<D, NST, ONCE, KINDS>(a, nxt, nxt.s.tile(nxt.i) * kTK + 16 * slab, id, kind, lds_slab + stage * S::STAGEB,
-                                            lds + slab * S::SLABB + stage * S::STAGEB, kg, vg);
-    if (kind == 0 && lane == 0) reinterpret_cast<unsigned*>(vis_s + stage)[slab] = bits;
-    id = page_id(a, nxt, nxt.s.tile(min(nxt.i + 1, nxt.T - 1)) * kTK + 16 * slab);
-  };
-  int id = page_id(a, nxt, nxt.s.tile(nxt.i) * kTK + 16 * slab);
-  issue(0, id);
-
-  int stage = 0, part_slot = 0;
-  while (f < f1) {
-    // ---- a unit
-    const Unit cur = nxt;
-    const int begin = cur.i, last_row = cur.s.q_len * a.g - 1;
-    const int wave_row = row_base + wave * WROWS;
-    const bool has_rows = wave_row <= last_row;
-    Rows<D, RB> w;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int R = min(wave_row + 16 * rb + l16, last_row), r = R / a.g, h = cur.kvh * a.g + R - r * a.g;
-      const uint16_t* qp = (const uint16_t*)a.q + cur.b * a.q_st[0] + h * a.q_st[1] + r * a.q_st[2];
-#pragma unroll
-      for (int s2 = 0; s2 < NS; ++s2) w.q[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
-      row_range(a, cur.s, r, w.lo[rb], w.hi[rb]);
-      w.neg_m[rb] = f32x4{0.f, 0.f, 0.f, 0.f}; w.thr[rb] = kNegBig; w.lsum[rb] = 0.f;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const Args a = arguments();
+    if constexpr (FLAT) {
+      if (a->min_tiles == 0) {                     // a workgroup per (sequence, K/V head)
+        open_unit<kTK>(nxt, blockIdx.x / a->Hkv, blockIdx.x % a->Hkv, 0);
+        left = nxt.T;
+      } else {
+        left = open_share<kTK>(blockIdx.x, nxt);
+      }
+    } else {
+      // The row tiles of a (sequence, K/V head, part), last rows first, run one after the other on one XCD, whose L2 brings them K and V
+      // once; heads that do not go round the XCDs evenly are cut into `cuts` lists of every so many-th row tile.
+      const int xcd = blockIdx.x % kNumXCDs, at = blockIdx.x / kNumXCDs, list = (a->row_tiles + a->cuts - 1) / a->cuts;
+      const int v = at / list * kNumXCDs + xcd, unit = v / a->cuts, rank = (at % list) * a->cuts + v % a->cuts;
+      if (unit >= a->B * a->Hkv * a->parts || rank >= a->row_tiles) return;
+      const int bh = unit / a->parts, part = unit - bh * a->parts;
+      nxt.b = bh / a->Hkv; nxt.kvh = bh - nxt.b * a->Hkv;
+      row_base = (a->row_tiles - 1 - rank) * (WROWS * NW);
+      const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
+      nxt.s = seen_by(a, lens[nxt.b], a->q_lens ? q_lens[nxt.b] : a->K, row_base / a->g, (row_base + WROWS * NW - 1) / a->g, kTK);
+      nxt.T = row_base < nxt.s.q_len * a->g ? max(nxt.s.tiles, 1) : 0;
+      const int per = max((nxt.T + a->parts - 1) / a->parts, a->min_tiles);
+      nxt.i = part * per;
+      left = min(per, nxt.T - nxt.i);
+      slot = (long long)bh * a->parts + part;
     }
-    // what the wave's rows see: all of them [all_lo, all_hi), any of them [any_lo, any_hi)
-    const int r0 = min(wave_row, last_row) / a.g, r1 = min(wave_row + WROWS - 1, last_row) / a.g;
-    int any_lo, all_hi, all_lo, any_hi;
-    row_range(a, cur.s, r0, any_lo, all_hi);
-    row_range(a, cur.s, r1, all_lo, any_hi);
+  }
+  if (left <= 0) return;
+  const Hot h = hot_arguments();
+  Pages pages;
+  pages.open(nxt.b);
+  BlockRows block;
+  block.open(nxt.b, nxt.kvh);
+
+  // LDS addresses of the lane's operands of slice 0 / d block 0 in stage 0; the others flip bits of them
+  const unsigned lds0 = uniform((int)(unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds);
+  const int e4 = l16 >> 2, c4 = l16 & 3, fv = (D == 128) ? 2 * (4 * (G & 1) + e4) : 2 * (2 * (G & 1) + (e4 >> 1));
+  const unsigned kro = lds0 + l16 * ROWB + ((G ^ ((D == 128) ? l16 : (l16 >> 1))) << 4);
+  const unsigned vro = lds0 + S::VB + (4 * G + e4) * ROWB + (((c4 >> 1) ^ fv) << 4) + ((c4 & 1) << 3);
+  const unsigned lds_slab = lds0 + slab * S::SLABB;
+
+  // Puts the tile at nxt in flight into ring stage `stage`; returns which of its keys some query row sees.  A tile that is not whole
+  // has landed on return (its transfers are not counted: step_wait).
+  auto issue = [&](int stage) -> unsigned long long {
+    const Seen& s = nxt.s;
+    if (s.tiles == 0) {
+      if (NST > 2) wait_transfers();
+      return 0;
+    }
+    const int k0 = s.tile(nxt.i) * kTK, k = k0 + 16 * slab;
+    pages.seek(h, k0);
+    const unsigned long long at = row_offset(h, pages.of(h, k), nxt.kvh, k, ROWB);
+    const unsigned to = lds_slab + stage * S::STAGEB;
+    if (pages.all_ok<kTK>(h, k0) && ((k0 >= s.lo && k0 + kTK - 16 <= s.last16) || k0 + kTK - 16 <= s.sink16)) {
+      if constexpr (NW == 8) {
+        if (kind == 0) move_slab<D, ONCE, false>(to, h.kp + at);
+        else move_slab<D, ONCE, true>(to + S::VB, h.vp + at);
+      } else {
+        move_slab<D, ONCE, false>(to, h.kp + at);
+        move_slab<D, ONCE, true>(to + S::VB, h.vp + at);
+      }
+      return ~0ull;
+    }
+    if (k0 >= s.n && k0 >= s.lo && k0 + kTK <= s.hi && block.k_stride != 0) {
+      const unsigned long long x = (unsigned)(k - s.n);
+      if (NW == 4 || kind == 0) move_strided<D, ONCE, false>(to, block.k + x * block.k_stride, block.k_stride);
+      if (NW == 4 || kind == 1) move_strided<D, ONCE, true>(to + S::VB, block.v + x * block.v_stride, block.v_stride);
+      return ~0ull;
+    }
+    const unsigned long long vis = seen_keys<kTK>(h, s, pages, k0);
+    const unsigned bits = (unsigned)(vis >> (16 * slab)) & 0xffffu;
+    unsigned char* const ptr = lds + slab * S::SLABB + stage * S::STAGEB;
+    if (NW == 4 || kind == 0) move_rows<D, ONCE, false>(s, nxt.b, nxt.kvh, k, bits, h.kp + at, to, ptr);
+    if (NW == 4 || kind == 1) move_rows<D, ONCE, true>(s, nxt.b, nxt.kvh, k, bits, h.vp + at, to + S::VB, ptr + S::VB);
+    if (NST > 2) wait_transfers();
+    return vis;
+  };
+  auto advance = [&]() {                           // nxt to the next tile of the share
+    if constexpr (FLAT) {
+      const int b = nxt.b, kvh = nxt.kvh;
+      next_tile<kTK>(nxt);
+      if (nxt.b != b) pages.open(nxt.b);
+      if (nxt.b != b || nxt.kvh != kvh) block.open(nxt.b, nxt.kvh);
+    } else {
+      ++nxt.i;
+    }
+  };
+  // Number of the last tile of which a value was taken out (values that are not finite, below); it only grows, so that a wave that
+  // reads it late sees a later tile's at worst
+  const lds_int_ptr flag = (lds_int_ptr)(uintptr_t)(lds0 + S::FLAG);
+  if (threadIdx.x == 0) *flag = 0;
+  wait_lds();
+  __builtin_amdgcn_s_barrier();
+  int number = 0;
+  // The ring: tile t is in stage t % NST; NST - 1 tiles are in flight ahead of the one being computed
+  unsigned long long vis[NST - 1];                 // of the tiles in flight, the oldest first
+  Unit cur = nxt;
+  vis[0] = issue(0);
+  if (NST > 2) {
+    vis[NST - 2] = 0;
+    if (left > 1) { advance(); vis[NST - 2] = issue(1); }
+  }
+
+  int stage = 0;
+  while (left > 0) {
+    // ---- a unit
+    const int begin = cur.i, wave_row = row_base + wave * WROWS;
+    Rows<D, RB> w;
+    bool has_rows;
+    int wg_hi, wg_lo;                              // keys that all of the workgroup's rows see: [wg_lo, wg_hi) as far as they exist
+    int any_lo, any_hi, all_lo, all_hi;            // what any / all of the wave's rows see
+    {
+      const Args a = arguments();
+      const int g = a->g, last_row = cur.s.q_len * g - 1;
+      has_rows = wave_row <= last_row;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int R = min(wave_row + 16 * rb + l16, last_row), r = R / g, hq = cur.kvh * g + R - r * g;
+        const uint16_t* qp = (const uint16_t*)a->q + cur.b * a->q_st[0] + hq * a->q_st[1] + r * a->q_st[2];
+#pragma unroll
+        for (int s2 = 0; s2 < NS; ++s2) w.q[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
+        w.pos[rb] = cur.s.N - cur.s.q_len + r;
+        w.neg_m[rb] = 0.f; w.thr[rb] = kNegBig; w.lsum[rb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      const int r0 = min(wave_row, last_row) / g, r1 = min(wave_row + WROWS - 1, last_row) / g;
+      row_range(a, cur.s, r0, any_lo, all_hi);
+      row_range(a, cur.s, r1, all_lo, any_hi);
+      if (!a->causal) all_hi = 0x7fffffff;         // what lies behind the last key is missing
+      wg_hi = a->causal ? cur.s.p0 + 1 : 0x7fffffff;
+      wg_lo = a->window > 0 ? cur.s.p1 - a->window + 1 : 0;
+    }
+    if (NST > 2) wait_transfers();                 // the query rows: no wait for them is left to the loop
+    bool redo = false;
     int i = begin;
-    while (i < cur.T && f < f1) {
-      wait_transfers();
+    while (i < cur.T && left > 0) {
+      // The tile has landed: transfers complete in order, and behind it at most those of one whole tile are in flight
+      if (NST > 2 && left > 1) {
+        asm volatile("" ::: "memory");
+        wait_vmcnt<Slab<D>::IPT>();
+        asm volatile("" ::: "memory");
+      } else {
+        wait_transfers();
+      }
+      // Rows at different positions and a tile that some see in part: the wave that moved a slab of V looks through it
+      const int k0 = cur.s.tile(i) * kTK;
+      const bool border = cur.s.p1 > cur.s.p0 && (k0 + kTK > wg_hi || (k0 < wg_lo && k0 + kTK > h.sinks));
+      ++number;
+      if (border && (NW == 4 || kind == 1)) {
+        const unsigned at = lds_slab + S::VB + stage * S::STAGEB + 16 * fresh_lane();
+        unsigned bad = 0;
+#pragma unroll
+        for (int t = 0; t < Slab<D>::IPT; ++t) bad |= nonfinite_bits((u32x4)*(lds_u32x4_ptr)(uintptr_t)(at + 1024 * t));
+        if (__builtin_expect(__ballot(bad != 0) != 0, 0)) {
+#pragma unroll
+          for (int t = 0; t < Slab<D>::IPT; ++t) {
+            const lds_u32x4_ptr p = (lds_u32x4_ptr)(uintptr_t)(at + 1024 * t);
+            *p = __builtin_bit_cast(u32x4, finite_part(__builtin_bit_cast(s16x8, (u32x4)*p)));
+          }
+          *flag = number;
+        }
+      }
       wait_lds();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      const bool more = f + 1 < f1;
-      const u32x4 seen = vis_s[stage];
-      if (more) {
-        if constexpr (FLAT) {
-          next_tile<kTK>(a, nxt);
-          if (nxt.i == 0) id = page_id(a, nxt, nxt.s.tile(0) * kTK + 16 * slab);
-        } else {
-          ++nxt.i;
-        }
-        issue(stage ^ 1, id);
+      if (border) redo |= uniform(*flag) >= number;
+      const unsigned long long seen = vis[0];
+      if (NST > 2) vis[0] = vis[NST - 2];
+      if (left > NST - 1) {
+        advance();
+        vis[NST - 2] = issue(stage == 0 ? NST - 1 : stage - 1);
       }
-      const int k0 = cur.s.tile(i) * kTK;
-      const u32x4 vb{(unsigned)uniform(seen[0]), (unsigned)uniform(seen[1]), (unsigned)uniform(seen[2]), (unsigned)uniform(seen[3])};
-      const bool any = (vb[0] | vb[1] | vb[2] | vb[3]) != 0, all = (vb[0] & vb[1] & vb[2] & vb[3]) == 0xffffu;
-      if (has_rows && any && k0 < any_hi && (k0 + kTK > any_lo || k0 < a.sinks)) {
-        const bool masked = !all || k0 + kTK > all_hi || (k0 < all_lo && k0 + kTK > a.sinks);
-        compute_tile<D, RB, NST>(a, w, lds, kro, vro, S::VB + stage * S::STAGEB, k0, masked, r1 > r0, vb);
-      }
-      ++i; ++f;
-      stage ^= 1;
-      kro ^= S::STAGEB;                            // (bits below a stage's size are those within a tile)
-      vro ^= S::STAGEB;
+      if (has_rows && seen != 0 && k0 < any_hi && (k0 + kTK > any_lo || k0 < h.sinks))
+        compute_tile<D, RB, NST>(h, w, kro + stage * S::STAGEB, vro + stage * S::STAGEB, k0, seen != ~0ull, k0 + kTK > all_hi,
+                                 k0 < all_lo && k0 + kTK > h.sinks, seen);
+      ++i; --left;
+      stage = stage == NST - 1 ? 0 : stage + 1;
     }
 
     // ---- this workgroup's share of the unit is done
+    const Args a = arguments();
     const bool whole = begin == 0 && i == cur.T;
+    const int g = a->g, last_row = cur.s.q_len * g - 1;
+    const long long slot0 = slot * a->R;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float l = w.lsum[rb];
@@ -369,8 +342,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
       if (R > last_row) continue;
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const int r = R / a.g, h = cur.kvh * a.g + R - r * a.g;
-        uint16_t* orow = (uint16_t*)a.out + cur.b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2];
+        const int r = R / g, hq = cur.kvh * g + R - r * g;
+        uint16_t* orow = (uint16_t*)a->out + cur.b * a->o_st[0] + hq * a->o_st[1] + r * a->o_st[2];
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
           uint2 x;
@@ -379,50 +352,54 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
           *reinterpret_cast<uint2*>(orow + 16 * db + 4 * G) = x;
         }
       } else {
-        const long long slot = (FLAT ? (long long)blockIdx.x * 2 + part_slot : slot_unit) * a.R + R;
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(a.ws_o + slot * D + 16 * db + 4 * G) = w.o[rb][db];
-        if (G == 0) { a.ws_ml[2 * slot] = w.thr[rb] == kNegBig ? kNegBig : -w.neg_m[rb][0]; a.ws_ml[2 * slot + 1] = l; }
+        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(a->ws_o + (slot0 + R) * D + 16 * db + 4 * G) = w.o[rb][db];
+        if (G == 0) { a->ws_ml[2 * (slot0 + R)] = w.thr[rb] == kNegBig ? kNegBig : -w.neg_m[rb]; a->ws_ml[2 * (slot0 + R) + 1] = l; }
       }
     }
-    part_slot = 1;
+    if (redo) redo_rows<D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, slot0);
+    if (FLAT) {
+      slot = 2LL * blockIdx.x + 1;                 // the first unit's partial result goes to slot 0, the last's to 1
+      if (left > 0) { cur.i = cur.T - 1; next_tile<kTK>(cur); }
+    }
   }
 }
 
 // Merges the parts of a row that a row tile's workgroups left, in the order of the keys: D / 4 lanes per row
 template <int D>
-__global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs a, int rows_wg) {
+__global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int rows_wg) {
+  const Args a = arguments();
   constexpr int TPR = D / 4, RPB = 256 / TPR;
   const long long at = (long long)blockIdx.x * RPB + threadIdx.x / TPR;
-  if (at >= (long long)a.B * a.Hkv * a.R) return;
-  const int bh = (int)(at / a.R), R = (int)(at - (long long)bh * a.R), b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+  if (at >= (long long)a->B * a->Hkv * a->R) return;
+  const int bh = (int)(at / a->R), R = (int)(at - (long long)bh * a->R), b = bh / a->Hkv, kvh = bh - b * a->Hkv;
   const int base = R / rows_wg * rows_wg;
-  const Seen s = seen_by(a, a.lens[b], a.q_lens ? a.q_lens[b] : a.K, base / a.g, (base + rows_wg - 1) / a.g, kTK);
-  if (R >= s.q_len * a.g) return;
-  const int T = max(s.tiles, 1), per = max((T + a.parts - 1) / a.parts, a.min_tiles), n = (T + per - 1) / per;
+  const Seen s = seen_by(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, base / a->g, (base + rows_wg - 1) / a->g, kTK);
+  if (R >= s.q_len * a->g) return;
+  const int T = max(s.tiles, 1), per = max((T + a->parts - 1) / a->parts, a->min_tiles), n = (T + per - 1) / per;
   if (n == 1) return;                              // written by its workgroup
   const int d = (threadIdx.x % TPR) * 4;
   float M = kNegBig, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int k = 0; k < n; ++k) {
-    const long long slot = ((long long)bh * a.parts + k) * a.R + R;
-    const f32x4 ov = *reinterpret_cast<const f32x4*>(a.ws_o + slot * D + d);
-    const float mk = a.ws_ml[2 * slot], lk = a.ws_ml[2 * slot + 1];
-    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a.scale_log2), c1 = exp2_fast((mk - up) * a.scale_log2);
+    const long long slot = ((long long)bh * a->parts + k) * a->R + R;
+    const f32x4 ov = *reinterpret_cast<const f32x4*>(a->ws_o + slot * D + d);
+    const float mk = a->ws_ml[2 * slot], lk = a->ws_ml[2 * slot + 1];
+    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
     acc = acc * c0 + ov * c1;
     l = l * c0 + lk * c1;
     M = up;
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int r = R / a.g, h = kvh * a.g + R - r * a.g;
+  const int r = R / a->g, h = kvh * a->g + R - r * a->g;
   uint2 w2;
   w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
   w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-  *reinterpret_cast<uint2*>((uint16_t*)a.out + b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2] + d) = w2;
+  *reinterpret_cast<uint2*>((uint16_t*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2] + d) = w2;
 }
 
 // ---- launch plan, from the parameters alone
-struct TilePlan { int rb, waves, flat, workers, parts, row_tiles, min_tiles; };
+struct TilePlan { int rb, waves, flat, workers, parts, row_tiles, cuts, min_tiles; };
 
 static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   const long long R = (long long)p.Hq / p.Hkv * p.K, units = (long long)p.B * p.Hkv;
@@ -458,6 +435,8 @@ static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   if (parts > most) parts = most;
   if (parts < 1) parts = 1;
   pl.parts = (int)parts;
+  pl.cuts = 1;
+  while (pl.cuts < kNumXCDs && (p.Hkv * parts * pl.cuts) % kNumXCDs != 0) pl.cuts *= 2;
   return pl;
 }
 
@@ -470,7 +449,7 @@ size_t paged_tile_workspace_bytes(const sdllm_paged_attn_params& p, bool with_bl
 
 template <int D, int RB, int NW, bool FLAT>
 static hipError_t launch_tile(const PagedArgs& a, unsigned grid, hipStream_t stream, bool launch) {
-  constexpr size_t bytes = TileShape<D, 2>::LDS;
+  constexpr size_t bytes = TileShape<D, NW == 8 ? 3 : 2>::LDS;
   static LdsOptIn st;
   hipError_t e = ensure_lds_opt_in(reinterpret_cast<const void*>(&paged_tile_kernel<D, RB, NW, FLAT>), bytes, st);
   if (e != hipSuccess || !launch) return e;
@@ -499,13 +478,15 @@ hipError_t prepare_paged_tile() {
 
 hipError_t launch_paged_tile(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
   const TilePlan pl = plan_tile(p, a.kb != nullptr);
-  a.workers = pl.workers; a.min_tiles = pl.min_tiles; a.parts = pl.parts; a.row_tiles = pl.row_tiles;
+  a.workers = pl.workers; a.min_tiles = pl.min_tiles; a.parts = pl.parts; a.row_tiles = pl.row_tiles; a.cuts = pl.cuts;
   const bool merge = pl.flat ? pl.min_tiles > 0 : pl.parts > 1;
   const size_t slots = pl.flat ? (size_t)pl.workers * 2 : (size_t)p.B * p.Hkv * pl.parts;
   a.ws_o = merge ? (float*)workspace : nullptr;
   a.ws_ml = merge ? a.ws_o + slots * a.R * p.D : nullptr;
-  const unsigned grid = pl.flat ? (unsigned)pl.workers : (unsigned)((long long)p.B * p.Hkv * pl.parts * pl.row_tiles);
-  hipError_t e = p.D == 128 ? launch_tile_d<128>(a, pl, grid, stream) : launch_tile_d<64>(a, pl, grid, stream);
+  long long grid = pl.workers;
+  if (!pl.flat)
+    grid = ((long long)p.B * p.Hkv * pl.parts * pl.cuts + kNumXCDs - 1) / kNumXCDs * kNumXCDs * ((pl.row_tiles + pl.cuts - 1) / pl.cuts);
+  hipError_t e = p.D == 128 ? launch_tile_d<128>(a, pl, (unsigned)grid, stream) : launch_tile_d<64>(a, pl, (unsigned)grid, stream);
   if (e != hipSuccess || !merge) return e;
   if (pl.flat) return launch_shares_merge(a, p.D, kTK, stream);
   const int rows_wg = 16 * pl.rb * pl.waves, rpb = 256 / (p.D / 4);
