@@ -38,7 +38,6 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
                                              bool below, unsigned long long vis) {
   using S = TileShape<D, NST>;
   constexpr int NS = S::NS, NDB = S::NDB;
-  __builtin_amdgcn_iglp_opt(0);                    // the compiler's interleaving of matrix instructions and LDS reads
   auto read_vt = [&](int db, int u) {
     const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)((vro ^ (db << 5)) + 32 * u * S::ROWB));
     const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(uintptr_t)((vro ^ (db << 5)) + (32 * u + 16) * S::ROWB));
@@ -50,14 +49,24 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) sacc[rb][kb] = f32x4{w.neg_m[rb], w.neg_m[rb], w.neg_m[rb], w.neg_m[rb]};
+  // all operand reads first, so that the products find theirs in registers one after the other
+  bf16x8 kop[4][NS];
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-    for (int s2 = 0; s2 < NS; ++s2) {
-      const bf16x8 kop = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
+    for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) sacc[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, w.q[rb][s2], sacc[rb][kb], 0, 0, 0);
-    }
+  for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+    for (int s2 = 0; s2 < NS; ++s2)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) sacc[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[kb][s2], w.q[rb][s2], sacc[rb][kb], 0, 0, 0);
+  // the values of the tile's first half travel under the softmax
+  s16x8 vop[2][NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) vop[0][db] = read_vt(db, 0);
+  __builtin_amdgcn_sched_barrier(0);
   if (missing || above || below) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) hide<4>(sacc[rb], k0, w.pos[rb] - h.window + 1, w.pos[rb] + 1, h.sinks, vis, missing, above, below);
@@ -121,18 +130,19 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   }
   // ---- O^T += V^T P^T
 #pragma unroll
+  for (int db = 0; db < NDB; ++db) vop[1][db] = read_vt(db, 1);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      const s16x8 vop = read_vt(db, u);
+    for (int db = 0; db < NDB; ++db)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
-        w.o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop), __builtin_bit_cast(bf16x8, pk[rb][u]), w.o[rb][db], 0, 0, 0);
-    }
+        w.o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop[u][db]), __builtin_bit_cast(bf16x8, pk[rb][u]), w.o[rb][db], 0, 0, 0);
 }
 
 template <int D, int RB, int NW, bool FLAT>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(PagedArgs) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tile_kernel(PagedArgs) {
   constexpr int NST = NW == 8 ? 3 : 2, WROWS = 16 * RB;
   constexpr bool ONCE = FLAT;                      // K/V is read by one workgroup only
   using S = TileShape<D, NST>;
@@ -191,15 +201,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
   // has landed on return (its transfers are not counted: step_wait).
   auto issue = [&](int stage) -> unsigned long long {
     const Seen& s = nxt.s;
-    if (s.tiles == 0) {
-      if (NST > 2) wait_transfers();
-      return 0;
-    }
     const int k0 = s.tile(nxt.i) * kTK, k = k0 + 16 * slab;
     pages.seek(h, k0);
     const unsigned long long at = row_offset(h, pages.of(h, k), nxt.kvh, k, ROWB);
     const unsigned to = lds_slab + stage * S::STAGEB;
-    if (pages.all_ok<kTK>(h, k0) && ((k0 >= s.lo && k0 + kTK - 16 <= s.last16) || k0 + kTK - 16 <= s.sink16)) {
+    if (s.tiles > 0 && pages.all_ok<kTK>(h, k0) && ((k0 >= s.lo && k0 + kTK - 16 <= s.last16) || k0 + kTK - 16 <= s.sink16)) {
       if constexpr (NW == 8) {
         if (kind == 0) move_slab<D, ONCE, false>(to, h.kp + at);
         else move_slab<D, ONCE, true>(to + S::VB, h.vp + at);
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
       if (NW == 4 || kind == 1) move_strided<D, ONCE, true>(to + S::VB, block.v + x * block.v_stride, block.v_stride);
       return ~0ull;
     }
-    const unsigned long long vis = seen_keys<kTK>(h, s, pages, k0);
+    const unsigned long long vis = seen_keys<kTK>(h, s, pages, k0);    // rows that see nothing: none
     const unsigned bits = (unsigned)(vis >> (16 * slab)) & 0xffffu;
     unsigned char* const ptr = lds + slab * S::SLABB + stage * S::STAGEB;
     if (NW == 4 || kind == 0) move_rows<D, ONCE, false>(s, nxt.b, nxt.kvh, k, bits, h.kp + at, to, ptr);
@@ -254,13 +260,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
     // ---- a unit
     const int begin = cur.i, wave_row = row_base + wave * WROWS;
     Rows<D, RB> w;
-    bool has_rows;
-    int wg_hi, wg_lo;                              // keys that all of the workgroup's rows see: [wg_lo, wg_hi) as far as they exist
-    int any_lo, any_hi, all_lo, all_hi;            // what any / all of the wave's rows see
+    int wg_hi, wg_lo;                              // ... of the workgroup's rows
+    int all_lo, all_hi;                            // keys that all of the wave's rows see: [all_lo, all_hi) as far as they exist
     {
       const Args a = arguments();
       const int g = a->g, last_row = cur.s.q_len * g - 1;
-      has_rows = wave_row <= last_row;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int R = min(wave_row + 16 * rb + l16, last_row), r = R / g, hq = cur.kvh * g + R - r * g;
@@ -273,9 +277,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
         for (int db = 0; db < NDB; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       const int r0 = min(wave_row, last_row) / g, r1 = min(wave_row + WROWS - 1, last_row) / g;
-      row_range(a, cur.s, r0, any_lo, all_hi);
-      row_range(a, cur.s, r1, all_lo, any_hi);
-      if (!a->causal) all_hi = 0x7fffffff;         // what lies behind the last key is missing
+      const int p0 = cur.s.N - cur.s.q_len;
+      all_hi = a->causal ? p0 + r0 + 1 : 0x7fffffff;
+      all_lo = a->window > 0 ? p0 + r1 - a->window + 1 : 0;
       wg_hi = a->causal ? cur.s.p0 + 1 : 0x7fffffff;
       wg_lo = a->window > 0 ? cur.s.p1 - a->window + 1 : 0;
     }
@@ -319,9 +323,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_tile_kernel(Pa
         advance();
         vis[NST - 2] = issue(stage == 0 ? NST - 1 : stage - 1);
       }
-      if (has_rows && seen != 0 && k0 < any_hi && (k0 + kTK > any_lo || k0 < h.sinks))
-        compute_tile<D, RB, NST>(h, w, kro + stage * S::STAGEB, vro + stage * S::STAGEB, k0, seen != ~0ull, k0 + kTK > all_hi,
-                                 k0 < all_lo && k0 + kTK > h.sinks, seen);
+      compute_tile<D, RB, NST>(h, w, kro + stage * S::STAGEB, vro + stage * S::STAGEB, k0, seen != ~0ull, k0 + kTK > all_hi,
+                               k0 < all_lo && k0 + kTK > h.sinks, seen);
       ++i; --left;
       stage = stage == NST - 1 ? 0 : stage + 1;
     }
