@@ -21,7 +21,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsdllm.so")
 SOURCES = ["api.hip", "kv_append.hip", "unmask.hip", "attention_f32.hip", "attention_bf16.hip", "rope.hip",
            "lm_head.hip", "probe.hip", "paged_api.hip", "paged_table.hip", "qk_norm_rope.hip", "paged_attention.hip",
-           "paged_attention_bf16.hip", "paged_attention_tile.hip"]
+           "paged_attention_bf16.hip", "paged_attention_tile.hip", "paged_attention_f32.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wno-inline-asm",
     # packed fp32 VALU forms are kept off for every HIP source of this build

@@ -12,8 +12,10 @@ struct PagedArgs {
   int B, Hq, Hkv, g, K, R;                         // R = g K: query rows of a (sequence, K/V head)
   int shift, n_pages, max_pages, max_kv, causal, window, sinks;
   unsigned page_bytes;                             // of one page, all heads
-  int workers, parts, row_tiles, cuts, min_tiles;  // how the key tiles are shared out (see the kernels)
-  float scale, scale_log2, thr8;                    // thr8: 8 in log2 units, as a difference of scores
+  int tile_rows, row_tiles;                        // query rows of a unit; units of a (sequence, K/V head)
+  int workers, parts, cuts, min_tiles;             // how the key tiles are shared out (see the kernels)
+  FastDiv by_g, by_row_tiles, by_Hkv;
+  float scale_log2, thr8;                          // thr8: 8 in log2 units, as a difference of scores
 };
 
 // The kernels read their arguments where they use them: a fresh pointer that the compiler cannot see through, in a scope of its own,
@@ -23,6 +25,13 @@ __device__ __forceinline__ Args arguments() {
   Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
   return p;
+}
+
+__device__ __forceinline__ int divide(int n, const __attribute__((address_space(4))) FastDiv& by) {
+  return (int)((__umulhi((unsigned)n, by.m) + (unsigned)n) >> by.s);
+}
+__device__ __forceinline__ long long quotient(long long n, long long d) {   // both >= 0; short where 32 bits do
+  return ((unsigned long long)(n | d) >> 32) == 0 ? (unsigned)n / (unsigned)d : n / d;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -90,12 +99,21 @@ __device__ __forceinline__ void wait_lds() {
   asm volatile("" ::: "memory");
 }
 
-// Key tiles of each sequence (over one K/V head), and the sum over the batch.  The lanes take 64 sequences at a time.
+// The call's units: row tile rt of sequence b (entry e = b row_tiles + rt), once for each K/V head.  What an entry sees:
 template <int TK>
-__device__ __forceinline__ int tiles_of(Args a, int b) {
-  if (b >= a->B) return 0;
-  const Seen s = seen_by(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, 0, a->K - 1, TK);
-  return s.q_len > 0 ? max(s.tiles, 1) : 0;        // rows that see nothing are a tile of their own: they are zero
+__device__ __forceinline__ Seen entry_seen(Args a, int n, int q_len, int rt) {
+  return seen_by(a, n, q_len, divide(rt * a->tile_rows, a->by_g), divide((rt + 1) * a->tile_rows - 1, a->by_g), TK);
+}
+__device__ __forceinline__ int tiles_to_do(Args a, const Seen& s, int rt) {
+  // rows that see nothing are a tile of their own: they are zero
+  return rt * a->tile_rows < s.q_len * a->g ? max(s.tiles, 1) : 0;
+}
+// Key tiles of each entry.  The lanes take 64 entries at a time.
+template <int TK>
+__device__ __forceinline__ int tiles_of(Args a, int e) {
+  if (e >= a->B * a->row_tiles) return 0;
+  const int b = divide(e, a->by_row_tiles), rt = e - b * a->row_tiles;
+  return tiles_to_do(a, entry_seen<TK>(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, rt), rt);
 }
 __device__ __forceinline__ int wave_scan(int v) {
 #pragma unroll
@@ -108,27 +126,27 @@ __device__ __forceinline__ int wave_scan(int v) {
 template <int TK>
 __device__ __forceinline__ long long all_tiles(Args a) {
   long long total = 0;
-  for (int b0 = 0; b0 < a->B; b0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, b0 + (int)(threadIdx.x & 63))), 63));
+  for (int e0 = 0; e0 < a->B * a->row_tiles; e0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, e0 + (int)(threadIdx.x & 63))), 63));
   return total * a->Hkv;
 }
 __device__ __forceinline__ long long tiles_per_worker(Args a, long long total) {
-  const long long n = (total + a->workers - 1) / a->workers;
+  const long long n = quotient(total + a->workers - 1, a->workers);
   return n > a->min_tiles ? n : a->min_tiles;
 }
 
-// A (sequence, K/V head) being walked; everything uniform
+// A unit being walked; everything uniform
 struct Unit {
-  int b, kvh, i, T;                                // tile i of T
+  int e, b, rt, kvh, i, T;                         // tile i of T
   Seen s;
 };
 
 template <int TK>
-__device__ __forceinline__ void open_unit(Unit& u, int b, int kvh, int i) {
+__device__ __forceinline__ void open_unit(Unit& u, int e, int kvh, int i) {
   const Args a = arguments();
-  u.b = b; u.kvh = kvh; u.i = i;
+  u.e = e; u.b = divide(e, a->by_row_tiles); u.rt = e - u.b * a->row_tiles; u.kvh = kvh; u.i = i;
   const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
-  u.s = seen_by(a, lens[b], a->q_lens ? q_lens[b] : a->K, 0, a->K - 1, TK);
-  u.T = u.s.q_len > 0 ? max(u.s.tiles, 1) : 0;
+  u.s = entry_seen<TK>(a, lens[u.b], a->q_lens ? q_lens[u.b] : a->K, u.rt);
+  u.T = tiles_to_do(a, u.s, u.rt);
 }
 
 // The unit and tile that the share of worker w begins with; returns the tiles of the share (0: none)
@@ -139,16 +157,16 @@ __device__ __forceinline__ int open_share(int w, Unit& u) {
   const long long total = all_tiles<TK>(a), per = tiles_per_worker(a, total), f = w * per;
   if (f >= total) return 0;
   long long before = 0;
-  for (int b0 = 0; b0 < a->B; b0 += 64) {
-    const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
+  for (int e0 = 0; e0 < a->B * a->row_tiles; e0 += 64) {
+    const int t = tiles_of<TK>(a, e0 + lane), upto = wave_scan(t);
     const int chunk = uniform(__shfl(upto, 63));
     if (f < before + (long long)chunk * a->Hkv) {
       const unsigned long long above = __ballot((long long)upto * a->Hkv > f - before);
       const int l = __builtin_ctzll(above);
-      const int tb = uniform(__shfl(t, l)), first = uniform(__shfl(upto, l)) - tb;
+      const int te = uniform(__shfl(t, l)), first = uniform(__shfl(upto, l)) - te;
       const long long rest = f - before - (long long)first * a->Hkv;
-      const int kvh = (int)(rest / tb);
-      open_unit<TK>(u, b0 + l, kvh, (int)(rest - (long long)kvh * tb));
+      const int kvh = (int)quotient(rest, te);
+      open_unit<TK>(u, e0 + l, kvh, (int)(rest - (long long)kvh * te));
       break;
     }
     before += (long long)chunk * a->Hkv;
@@ -160,8 +178,8 @@ __device__ __forceinline__ void next_tile(Unit& u) {
   if (++u.i < u.T) return;
   const Args a = arguments();
   if (u.kvh + 1 < a->Hkv) { ++u.kvh; u.i = 0; return; }
-  int b = u.b;
-  do { open_unit<TK>(u, ++b, 0, 0); } while (u.T == 0 && b + 1 < a->B);
+  int e = u.e;
+  do { open_unit<TK>(u, ++e, 0, 0); } while (u.T == 0 && e + 1 < a->B * a->row_tiles);
 }
 
 // What the loop over tiles needs of the arguments
@@ -347,9 +365,15 @@ __device__ __forceinline__ s16x8 finite_part(const s16x8& v) {
   return __builtin_bit_cast(s16x8, x);
 }
 
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((unsigned)x << 16); }
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(uint16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }
+
 // Rows R0 .. R0 + count - 1 of a unit over its tiles [i0, i1), one row after the other: a lane per key, then a lane per column.  Where the
-// result is finite, what the caller has written stands; else it is written again, as a row of the output or as a partial result.
-template <int D, int TK>
+// result is finite, what the caller has written stands; else it is written again, as a row of the output or as a partial result
+// (slot0: that of row 0).
+template <typename T, int D, int TK>
 __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0, int i1, int R0, int count, bool whole,
                                           long long slot0) {
   const Args a = arguments();
@@ -357,8 +381,8 @@ __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0,
   wait_transfers();                                // what the caller has written is in front of what is written here
 #pragma unroll 1
   for (int R = R0; R < min(R0 + count, s.q_len * a->g); ++R) {
-    const int r = R / a->g, h = kvh * a->g + R - r * a->g;
-    const uint16_t* q = (const uint16_t*)a->q + b * a->q_st[0] + h * a->q_st[1] + r * a->q_st[2];
+    const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
+    const T* q = (const T*)a->q + b * a->q_st[0] + h * a->q_st[1] + r * a->q_st[2];
     int lo, hi;
     row_range(a, s, r, lo, hi);
     float m = kNegBig, l = 0.f, o[D / 64] = {};
@@ -366,23 +390,23 @@ __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0,
     for (int i = i0; i < i1; ++i) {
       const int key = s.tile(i) * TK + lane;
       bool sees = (lane < TK) & (key < hi) & ((key >= lo) | (key < a->sinks));
-      const uint16_t *k = nullptr, *v = nullptr;
+      const T *k = nullptr, *v = nullptr;
       if (sees) {
         if (key < s.n) {
           const int page = a->table[(long long)b * a->max_pages + (key >> a->shift)];
           sees = (unsigned)page < (unsigned)a->n_pages;
           const long long at = ((((long long)page * a->Hkv + kvh) << a->shift) + (key & ((1 << a->shift) - 1))) * D;
-          k = (const uint16_t*)a->kp + at; v = (const uint16_t*)a->vp + at;
+          k = (const T*)a->kp + at; v = (const T*)a->vp + at;
         } else {
-          k = (const uint16_t*)a->kb + b * a->kb_st[0] + kvh * a->kb_st[1] + (key - s.n) * a->kb_st[2];
-          v = (const uint16_t*)a->vb + b * a->vb_st[0] + kvh * a->vb_st[1] + (key - s.n) * a->vb_st[2];
+          k = (const T*)a->kb + b * a->kb_st[0] + kvh * a->kb_st[1] + (key - s.n) * a->kb_st[2];
+          v = (const T*)a->vb + b * a->vb_st[0] + kvh * a->vb_st[1] + (key - s.n) * a->vb_st[2];
         }
       }
       float z = -INFINITY;
       if (sees) {
         z = 0.f;
 #pragma unroll 1
-        for (int d = 0; d < D; ++d) z = fmaf(__uint_as_float((unsigned)q[d] << 16), __uint_as_float((unsigned)k[d] << 16), z);
+        for (int d = 0; d < D; ++d) z = fmaf(to_float(q[d]), to_float(k[d]), z);
       }
       float mx = z;
 #pragma unroll
@@ -397,9 +421,9 @@ __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0,
       for (unsigned long long left = __ballot(sees); left != 0; left &= left - 1) {
         const int j = __builtin_ctzll(left);
         const float pj = __shfl(p, j);
-        const uint16_t* vj = (const uint16_t*)(uintptr_t)__shfl((unsigned long long)(uintptr_t)v, j);
+        const T* vj = (const T*)(uintptr_t)__shfl((unsigned long long)(uintptr_t)v, j);
 #pragma unroll
-        for (int u = 0; u < D / 64; ++u) o[u] = fmaf(pj, __uint_as_float((unsigned)vj[lane + 64 * u] << 16), o[u]);
+        for (int u = 0; u < D / 64; ++u) o[u] = fmaf(pj, to_float(vj[lane + 64 * u]), o[u]);
       }
     }
     bool finite = true;
@@ -407,9 +431,9 @@ __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0,
     for (int u = 0; u < D / 64; ++u) finite &= __builtin_isfinite(o[u]);
     if (__ballot(!finite) == 0) continue;
     if (whole) {
-      uint16_t* out = (uint16_t*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2];
+      T* out = (T*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2];
 #pragma unroll
-      for (int u = 0; u < D / 64; ++u) out[lane + 64 * u] = __builtin_bit_cast(uint16_t, (__bf16)(o[u] / l));
+      for (int u = 0; u < D / 64; ++u) put(out + lane + 64 * u, o[u] / l);
     } else {
 #pragma unroll
       for (int u = 0; u < D / 64; ++u) a->ws_o[(slot0 + R) * D + lane + 64 * u] = o[u];
@@ -418,11 +442,21 @@ __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0,
   }
 }
 
-// Kernels by query rows per (sequence, K/V head): up to 32 (stream), more (tile); both bf16
+// Kernels: bf16 by query rows per (sequence, K/V head), up to 32 (stream) and more (tile); fp32
 size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block);
 hipError_t launch_paged_stream(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream);
 size_t paged_tile_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block);
 hipError_t launch_paged_tile(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream);
-hipError_t launch_shares_merge(const PagedArgs& a, int D, int TK, hipStream_t stream);
+size_t paged_f32_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block);
+hipError_t launch_paged_f32(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream);
+
+// Most key tiles of TK that a unit of `rows` query rows can have
+long long paged_most_tiles(const sdllm_paged_attn_params& p, bool with_block, long long rows, int TK);
+// Units in equal shares: workers, tiles of a share at least, 0: a worker per unit and no merge
+struct SharePlan { int workers, min_tiles; };
+SharePlan plan_shares(const sdllm_paged_attn_params& p, bool with_block, int tile_rows, int row_tiles, int TK, int at_once, int min_tiles);
+size_t share_bytes(const SharePlan& pl, int tile_rows, int D);
+void set_shares(PagedArgs& a, const SharePlan& pl, int tile_rows, int row_tiles, int D, void* workspace);
+hipError_t launch_shares_merge(const PagedArgs& a, int dtype, int D, int TK, hipStream_t stream);
 
 }  // namespace sdllm

@@ -1,89 +1,161 @@
-// Attention over a paged K/V cache (sdllm_paged_attention): one wave per query row.  Visible keys are [0, sinks) and [lo, hi); a
-// wave takes 64 of them at a time, a lane the score of one, then a lane the output columns.
+// sdllm_paged_attention: dispatch, the plan by equal shares that its kernels have in common, and the merge of the shares.
 #include "paged_attention.h"
+#include <cmath>
 
 namespace sdllm {
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((unsigned)x << 16); }
-__device__ __forceinline__ void store(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store(uint16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }
-
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_attention_row_kernel(PagedArgs a) {
-  __shared__ float q_s[4][D], p_s[4][64];
-  __shared__ long long v_s[4][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long row = (long long)blockIdx.x * 4 + wave;
-  if (row >= (long long)a.B * a.Hq * a.K) return;
-  const int r = (int)(row % a.K);
-  const int h = (int)(row / a.K % a.Hq), b = (int)(row / a.K / a.Hq);
-  const int q_len = a.q_lens ? min(max(a.q_lens[b], 0), a.K) : a.K;
-  if (r >= q_len) return;
-  const int n = min(max(a.lens[b], 0), a.max_kv), N = n + (a.kb ? q_len : 0), kvh = h / a.g;
-  const int p = N - q_len + r;
-  const int hi = a.causal ? max(min(p + 1, N), 0) : N;
-  const int lo = a.window ? min(max(p - a.window + 1, 0), hi) : 0;
-  const int first = min(a.sinks, lo), count = first + hi - lo;
-  const T* q = (const T*)a.q + b * a.q_st[0] + h * a.q_st[1] + r * a.q_st[2];
-  for (int d = lane; d < D; d += 64) q_s[wave][d] = to_float(q[d]) * a.scale;
-  float m = -3.0e38f, l = 0.f, o[D / 64];
-#pragma unroll
-  for (int u = 0; u < D / 64; ++u) o[u] = 0.f;
-  for (int i0 = 0; i0 < count; i0 += 64) {
-    const int i = i0 + lane;
-    float s = -INFINITY;
-    const T* vrow = nullptr;
-    if (i < count) {
-      const int key = i < first ? i : lo + i - first;
-      const T* krow = nullptr;
-      if (key < n) {
-        const int page = a.table[(long long)b * a.max_pages + (key >> a.shift)];
-        if ((unsigned)page < (unsigned)a.n_pages) {
-          const long long at = ((((long long)page * a.Hkv + kvh) << a.shift) + (key & ((1 << a.shift) - 1))) * D;
-          krow = (const T*)a.kp + at; vrow = (const T*)a.vp + at;
-        }
-      } else {
-        krow = (const T*)a.kb + b * a.kb_st[0] + kvh * a.kb_st[1] + (key - n) * a.kb_st[2];
-        vrow = (const T*)a.vb + b * a.vb_st[0] + kvh * a.vb_st[1] + (key - n) * a.vb_st[2];
-      }
-      if (krow) {
-        s = 0.f;
-        for (int d = 0; d < D; ++d) s = fmaf(q_s[wave][d], to_float(krow[d]), s);
-      }
+// Merges the shares of every output row that several workers walked, in the order of the tiles.  GROUPS groups of D / 4 lanes take
+// every so many-th share of a row, then one adds up the groups, in order: one group per row where there are many rows (a
+// workgroup then merges several), else a workgroup per row.
+template <typename T, int D, int TK, int GROUPS>
+__global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
+  const Args a = arguments();
+  constexpr int TPR = D / 4, RPW = 256 / (TPR * GROUPS);
+  __shared__ f32x4 o_s[GROUPS > 1 ? GROUPS : 1][TPR];
+  __shared__ float m_s[GROUPS], l_s[GROUPS];
+  const int lane = threadIdx.x & 63, grp = threadIdx.x / TPR % GROUPS, d = threadIdx.x % TPR * 4;
+  // the rows of a workgroup: of one (sequence, K/V head, row tile)
+  const int per_tile = (a->tile_rows + RPW - 1) / RPW;
+  const unsigned tile = blockIdx.x / (unsigned)per_tile;
+  const int e = divide(tile, a->by_Hkv), kvh = tile - e * a->Hkv, b = divide(e, a->by_row_tiles), rt = e - b * a->row_tiles;
+  const int row = (blockIdx.x - tile * per_tile) * RPW + threadIdx.x / (TPR * GROUPS), R = rt * a->tile_rows + row;
+  // where the unit's tiles lie among the call's
+  long long total = 0, start = 0;
+  int n = 0;
+  for (int e0 = 0; e0 < a->B * a->row_tiles; e0 += 64) {
+    const int t = tiles_of<TK>(a, e0 + lane), upto = wave_scan(t);
+    if (e >= e0 && e < e0 + 64) {
+      n = uniform(__shfl(t, e - e0));
+      start = (total + uniform(__shfl(upto, e - e0)) - n) * a->Hkv + (long long)kvh * n;
     }
-    float mx = s;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    const float m_new = fmaxf(m, mx), corr = expf(m - m_new), w = expf(s - m_new);
-    float sum = w;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    m = m_new;
-    l = l * corr + sum;
-#pragma unroll
-    for (int u = 0; u < D / 64; ++u) o[u] *= corr;
-    p_s[wave][lane] = w;
-    v_s[wave][lane] = (long long)(uintptr_t)vrow;
-    __builtin_amdgcn_wave_barrier();
-    for (int j = 0; j < min(64, count - i0); ++j) {
-      const T* vr = (const T*)(uintptr_t)v_s[wave][j];
-      if (!vr) continue;
-      const float w2 = p_s[wave][j];
-#pragma unroll
-      for (int u = 0; u < D / 64; ++u) o[u] = fmaf(w2, to_float(vr[lane + 64 * u]), o[u]);
-    }
-    __builtin_amdgcn_wave_barrier();
+    total += uniform(__shfl(upto, 63));
   }
-  T* out = (T*)a.out + b * a.o_st[0] + h * a.o_st[1] + r * a.o_st[2];
+  total *= a->Hkv;
+  if (n == 0) return;
+  const long long per = tiles_per_worker(a, total);
+  const int w0 = (int)quotient(start, per), w1 = (int)quotient(start + n - 1, per);
+  if (w0 == w1) return;                            // written by its worker
+  const int q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
+  const bool exists = row < a->tile_rows && R < q_len * a->g;
+  float M = kNegBig, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float mk, float lk, const f32x4& ov) {
+    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
+    acc = acc * c0 + ov * c1;
+    l = l * c0 + lk * c1;
+    M = up;
+  };
+  if (exists) {
+    // a unit is its worker's first one unless the worker began before it
+    auto slot = [&](int w) { return ((long long)w * 2 + (start > w * per ? 1 : 0)) * a->tile_rows + row; };
+    int w = w0 + grp;
+    for (; w + 3 * GROUPS <= w1; w += 4 * GROUPS) {            // four shares' loads together
+      f32x4 ov[4]; float mk[4], lk[4];
 #pragma unroll
-  for (int u = 0; u < D / 64; ++u) store(out + lane + 64 * u, l == 0.f ? 0.f : o[u] / l);
+      for (int u = 0; u < 4; ++u) {
+        const long long at = slot(w + u * GROUPS);
+        ov[u] = *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d);
+        mk[u] = a->ws_ml[2 * at]; lk[u] = a->ws_ml[2 * at + 1];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add(mk[u], lk[u], ov[u]);
+    }
+    for (; w <= w1; w += GROUPS) {
+      const long long at = slot(w);
+      add(a->ws_ml[2 * at], a->ws_ml[2 * at + 1], *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d));
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    o_s[grp][threadIdx.x % TPR] = acc;
+    if (d == 0) { m_s[grp] = M; l_s[grp] = l; }
+    __syncthreads();
+    if (grp != 0) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) add(m_s[k], l_s[k], o_s[k][threadIdx.x % TPR]);
+  }
+  if (!exists) return;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
+  T* out = (T*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2] + d;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(out) = acc * inv;
+  } else {
+    uint2 w2;
+    w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+    *reinterpret_cast<uint2*>(out) = w2;
+  }
+}
+
+// Rows up to which each has a workgroup of its own: that many are on the chip at once, and what counts is the way through a row's
+// shares.  With more rows it is the number of workgroups.  (32 query heads, one row each, over 32768 keys: 35 us with the attention
+// itself, 67 with all rows in 128 workgroups; 28 heads of 32 rows for 8 sequences of 4096 keys: 55 and 48.)
+constexpr int kMergeAlone = 8 * kNumCUs;
+
+template <typename T, int D, int TK>
+static void launch_merge(const PagedArgs& a, hipStream_t stream) {
+  constexpr int all = 256 / (D / 4);
+  const long long units = (long long)a.B * a.Hkv * a.row_tiles;
+  if (units * a.tile_rows <= kMergeAlone) {
+    hipLaunchKernelGGL((shares_merge_kernel<T, D, TK, all>), dim3((unsigned)(units * a.tile_rows)), dim3(256), 0, stream, a);
+  } else {
+    const int per_tile = (a.tile_rows + all - 1) / all;
+    hipLaunchKernelGGL((shares_merge_kernel<T, D, TK, 1>), dim3((unsigned)(units * per_tile)), dim3(256), 0, stream, a);
+  }
+}
+
+hipError_t launch_shares_merge(const PagedArgs& a, int dtype, int D, int TK, hipStream_t stream) {
+  if (dtype == SDLLM_FP32) {
+    if (D == 128) launch_merge<float, 128, 16>(a, stream);
+    else launch_merge<float, 64, 16>(a, stream);
+  } else if (D == 64) {
+    launch_merge<uint16_t, 64, 64>(a, stream);
+  } else if (TK == 32) {
+    launch_merge<uint16_t, 128, 32>(a, stream);
+  } else {
+    launch_merge<uint16_t, 128, 64>(a, stream);
+  }
+  return hipGetLastError();
+}
+
+long long paged_most_tiles(const sdllm_paged_attn_params& p, bool with_block, long long rows, int TK) {
+  const long long N = p.max_kv_len + (with_block ? p.K : 0), g = p.Hq / p.Hkv;
+  long long tiles = (N + TK - 1) / TK;
+  if (p.window > 0) {
+    const long long span = (rows + g - 1) / g;     // positions of the rows
+    const long long seen = ((long long)p.window + (span < p.K ? span : p.K) + TK - 2) / TK + 1 + ((long long)p.sinks + TK - 1) / TK;
+    const long long behind = p.causal ? 0 : ((long long)p.K + TK - 1) / TK;
+    if (seen + behind < tiles) tiles = seen + behind;
+  }
+  return tiles < 1 ? 1 : tiles;
+}
+
+SharePlan plan_shares(const sdllm_paged_attn_params& p, bool with_block, int tile_rows, int row_tiles, int TK, int at_once, int min_tiles) {
+  const long long units = (long long)p.B * p.Hkv * row_tiles, tiles = paged_most_tiles(p, with_block, tile_rows, TK);
+  const long long per = p.kv_splits > 0 ? (tiles + p.kv_splits - 1) / p.kv_splits : min_tiles;
+  // A worker per unit where a unit is one share anyway, where the units go round all workers several times, and where finding the
+  // shares (a walk over the batch's lengths) or the merge's grid would get long
+  if (p.kv_splits == 1 || tiles <= per || units * tile_rows >= (1 << 23) || (p.kv_splits == 0 && (units >= 2LL * at_once || (long long)p.B * row_tiles > 2048)))
+    return SharePlan{(int)units, 0};
+  const long long w = (units * tiles + per - 1) / per, most = p.kv_splits > 0 ? 1 << 18 : at_once;
+  return SharePlan{(int)(w < most ? w : most), (int)per};
+}
+
+size_t share_bytes(const SharePlan& pl, int tile_rows, int D) {
+  return pl.min_tiles == 0 ? 0 : (size_t)pl.workers * 2 * tile_rows * (D + 2) * sizeof(float);
+}
+
+void set_shares(PagedArgs& a, const SharePlan& pl, int tile_rows, int row_tiles, int D, void* workspace) {
+  a.tile_rows = tile_rows; a.row_tiles = row_tiles; a.by_row_tiles = FastDiv(row_tiles);
+  a.workers = pl.workers; a.min_tiles = pl.min_tiles;
+  a.ws_o = pl.min_tiles ? (float*)workspace : nullptr;
+  a.ws_ml = pl.min_tiles ? a.ws_o + (size_t)pl.workers * 2 * tile_rows * D : nullptr;
 }
 
 static bool few_rows(const sdllm_paged_attn_params& p) { return (long long)p.Hq / p.Hkv * p.K <= 32; }
 
 size_t paged_attention_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
-  if (p.dtype == SDLLM_FP32) return 0;
+  if (p.dtype == SDLLM_FP32) return paged_f32_workspace_bytes(p, with_block);
   return few_rows(p) ? paged_stream_workspace_bytes(p, with_block) : paged_tile_workspace_bytes(p, with_block);
 }
 
@@ -97,22 +169,20 @@ static void dense_or(const int64_t* given, int H, int K, int D, long long* out) 
 hipError_t launch_paged_attention(const sdllm_paged_attn_params& p, const void* q, const void* k_pages, const void* v_pages,
                                   const int32_t* table, const int32_t* lens, const void* k_block, const void* v_block,
                                   const int32_t* q_lens, void* out, void* workspace, hipStream_t stream) {
-  PagedArgs a;
+  PagedArgs a{};
   a.q = q; a.kp = k_pages; a.vp = v_pages; a.table = table; a.lens = lens; a.kb = k_block; a.vb = v_block; a.q_lens = q_lens; a.out = out;
   dense_or(p.q_stride, p.Hq, p.K, p.D, a.q_st);
   dense_or(p.out_stride, p.Hq, p.K, p.D, a.o_st);
   dense_or(p.k_block_stride, p.Hkv, p.K, p.D, a.kb_st);
   dense_or(p.v_block_stride, p.Hkv, p.K, p.D, a.vb_st);
-  a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.R = a.g * p.K; a.shift = __builtin_ctz(p.page_size); a.page_bytes = (unsigned)((long long)p.Hkv * p.page_size * p.D * 2);
+  a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.R = a.g * p.K;
+  a.shift = __builtin_ctz(p.page_size); a.page_bytes = (unsigned)((long long)p.Hkv * p.page_size * p.D * (p.dtype == SDLLM_FP32 ? 4 : 2));
   a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.max_kv = p.max_kv_len; a.causal = p.causal; a.window = p.window; a.sinks = p.sinks;
-  a.scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.D);
-  a.scale_log2 = a.scale * kLog2e; a.thr8 = 8.0f / a.scale_log2;
-  if (p.dtype == SDLLM_BF16) return few_rows(p) ? launch_paged_stream(p, a, workspace, stream) : launch_paged_tile(p, a, workspace, stream);
-  const long long rows = (long long)p.B * p.Hq * p.K;
-  const dim3 grid((unsigned)((rows + 3) / 4));
-  if (p.D == 64) hipLaunchKernelGGL((paged_attention_row_kernel<float, 64>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((paged_attention_row_kernel<float, 128>), grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
+  a.by_g = FastDiv(a.g); a.by_Hkv = FastDiv(a.Hkv);
+  const float scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.D);
+  a.scale_log2 = scale * kLog2e; a.thr8 = 8.0f / a.scale_log2;
+  if (p.dtype == SDLLM_FP32) return launch_paged_f32(p, a, workspace, stream);
+  return few_rows(p) ? launch_paged_stream(p, a, workspace, stream) : launch_paged_tile(p, a, workspace, stream);
 }
 
 }  // namespace sdllm

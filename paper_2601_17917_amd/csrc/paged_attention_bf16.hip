@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
     const Args a = arguments();
     if (worker >= a->workers) return;
     if (a->min_tiles == 0) {                       // a wave per (sequence, K/V head)
-      open_unit<TK>(nxt, worker / a->Hkv, worker % a->Hkv, 0);
+      const int e = divide(worker, a->by_Hkv);
+      open_unit<TK>(nxt, e, worker - e * a->Hkv, 0);
       left = nxt.T;
     } else {
       left = open_share<TK>(worker, nxt);
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
       const int g = a->g, last_row = cur.s.q_len * g - 1;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const int R = min(16 * rb + l16, last_row), r = R / g, hq = cur.kvh * g + R - r * g;
+        const int R = min(16 * rb + l16, last_row), r = divide(R, a->by_g), hq = cur.kvh * g + R - r * g;
         const uint16_t* qp = (const uint16_t*)a->q + cur.b * a->q_st[0] + hq * a->q_st[1] + r * a->q_st[2];
 #pragma unroll
         for (int s2 = 0; s2 < NS; ++s2) qreg[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
       if (R > last_row) continue;
       if (whole) {
         const float inv = lsum[rb] == 0.f ? 0.f : 1.0f / lsum[rb];
-        const int r = R / g, hq = cur.kvh * g + R - r * g;
+        const int r = divide(R, a->by_g), hq = cur.kvh * g + R - r * g;
         uint16_t* orow = (uint16_t*)a->out + cur.b * a->o_st[0] + hq * a->o_st[1] + r * a->o_st[2];
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
@@ -264,131 +265,36 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
         if (G == 0) { a->ws_ml[2 * (slot0 + R)] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; a->ws_ml[2 * (slot0 + R) + 1] = lsum[rb]; }
       }
     }
-    if (redo) redo_rows<D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, slot0);
+    if (redo) redo_rows<uint16_t, D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, slot0);
     part = 1;
   }
 }
 
-// Merges the shares of every output row that several workers (waves here, workgroups of the tile kernel) walked, in the order of the tiles.  A workgroup per row: 256 / (D / 4)
-// groups of lanes take every so many-th share, then one adds up the groups, in order.
-template <int D, int TK>
-__global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
-  const Args a = arguments();
-  constexpr int TPR = D / 4, NG = 256 / TPR;
-  __shared__ f32x4 o_s[NG][TPR];
-  __shared__ float m_s[NG], l_s[NG];
-  const unsigned unit = blockIdx.x / (unsigned)a->R;
-  const int R = blockIdx.x - unit * a->R, b = unit / (unsigned)a->Hkv, kvh = unit - b * a->Hkv;
-  // where the unit's tiles lie among the call's
-  const int lane = threadIdx.x & 63;
-  long long total = 0, start = 0;
-  int T = 0, q_len = 0;
-  for (int b0 = 0; b0 < a->B; b0 += 64) {
-    const int t = tiles_of<TK>(a, b0 + lane), upto = wave_scan(t);
-    if (b >= b0 && b < b0 + 64) {
-      T = uniform(__shfl(t, b - b0));
-      start = (total + uniform(__shfl(upto, b - b0)) - T) * a->Hkv + (long long)kvh * T;
-    }
-    total += uniform(__shfl(upto, 63));
-  }
-  total *= a->Hkv;
-  q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
-  if (T == 0 || R >= q_len * a->g) return;
-  const long long per = tiles_per_worker(a, total);
-  const int w0 = (int)(start / per), w1 = (int)((start + T - 1) / per);
-  if (w0 == w1) return;                            // written by its wave
-  const int grp = threadIdx.x / TPR, d = (threadIdx.x % TPR) * 4;
-  float M = kNegBig, l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int w = w0 + grp; w <= w1; w += NG) {
-    // the unit is its wave's first one unless the wave began before it
-    const long long slot = ((long long)w * 2 + (start > w * per ? 1 : 0)) * a->R + R;
-    const f32x4 ov = *reinterpret_cast<const f32x4*>(a->ws_o + slot * D + d);
-    const float mk = a->ws_ml[2 * slot], lk = a->ws_ml[2 * slot + 1];
-    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
-    acc = acc * c0 + ov * c1;
-    l = l * c0 + lk * c1;
-    M = up;
-  }
-  o_s[grp][threadIdx.x % TPR] = acc;
-  if (d == 0) { m_s[grp] = M; l_s[grp] = l; }
-  __syncthreads();
-  if (grp != 0) return;
-#pragma unroll
-  for (int k = 1; k < NG; ++k) {
-    const float up = fmaxf(M, m_s[k]), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((m_s[k] - up) * a->scale_log2);
-    acc = acc * c0 + o_s[k][threadIdx.x % TPR] * c1;
-    l = l * c0 + l_s[k] * c1;
-    M = up;
-  }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int r = R / a->g, h = kvh * a->g + R - r * a->g;
-  uint2 w2;
-  w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-  w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-  *reinterpret_cast<uint2*>((uint16_t*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2] + d) = w2;
-}
+static constexpr int kStreamWaves = 8 * kNumCUs;   // resident at once: two workgroups of 64 KiB per CU
+static constexpr int kStreamMinTiles = 2;
 
-// ---- launch plan, from the parameters alone
-constexpr int kStreamWaves = 8 * kNumCUs;          // resident at once: two workgroups of 64 KiB per CU
-constexpr int kStreamMinTiles = 2;
-constexpr int kStreamMaxRows = 32;
-
-struct StreamPlan { int workers, min_tiles; bool merge; };
-
-static StreamPlan plan_stream(const sdllm_paged_attn_params& p, bool with_block) {
-  const long long TK = 4096 / p.D, units = (long long)p.B * p.Hkv;
-  const long long N = p.max_kv_len + (with_block ? p.K : 0);
-  long long tiles = (N + TK - 1) / TK;             // most a unit can have
-  if (p.window > 0) {
-    const long long seen = (p.window + p.K + TK - 2) / TK + 1 + (p.sinks + TK - 1) / TK;
-    if (seen < tiles) tiles = seen;
-  }
-  if (tiles < 1) tiles = 1;
-  StreamPlan pl;
-  long long per = kStreamMinTiles;
-  if (p.kv_splits > 0) per = (tiles + p.kv_splits - 1) / p.kv_splits;
-  pl.merge = !(p.kv_splits == 1 || units * (p.Hq / p.Hkv) * p.K >= (1 << 24) || (p.kv_splits == 0 && (units >= 2 * kStreamWaves || p.B > 1024 || tiles <= per)));
-  if (!pl.merge) {
-    pl.workers = (int)units; pl.min_tiles = 0;
-    return pl;
-  }
-  pl.min_tiles = (int)per;
-  long long w = (units * tiles + per - 1) / per;
-  const long long most = p.kv_splits > 0 ? 1 << 20 : kStreamWaves;
-  pl.workers = (int)(w < most ? w : most);
-  return pl;
+static SharePlan plan_stream(const sdllm_paged_attn_params& p, bool with_block) {
+  return plan_shares(p, with_block, p.Hq / p.Hkv * p.K, 1, 4096 / p.D, kStreamWaves, kStreamMinTiles);
 }
 
 size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
-  const StreamPlan pl = plan_stream(p, with_block);
-  return pl.merge ? (size_t)pl.workers * 2 * (size_t)(p.Hq / p.Hkv) * p.K * (p.D + 2) * sizeof(float) : 0;
-}
-
-hipError_t launch_shares_merge(const PagedArgs& a, int D, int TK, hipStream_t stream) {
-  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.R));
-  if (D == 64) hipLaunchKernelGGL((shares_merge_kernel<64, 64>), grid, dim3(256), 0, stream, a);
-  else if (TK == 32) hipLaunchKernelGGL((shares_merge_kernel<128, 32>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((shares_merge_kernel<128, 64>), grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
+  return share_bytes(plan_stream(p, with_block), p.Hq / p.Hkv * p.K, p.D);
 }
 
 template <int D>
-static hipError_t launch_stream(const PagedArgs& a, const StreamPlan& pl, hipStream_t stream) {
-  const dim3 grid((pl.workers + 3) / 4);
+static void launch_stream(const PagedArgs& a, hipStream_t stream) {
+  const dim3 grid((a.workers + 3) / 4);
   if (a.R <= 16) hipLaunchKernelGGL((paged_stream_kernel<D, 1>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((paged_stream_kernel<D, 2>), grid, dim3(256), 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !pl.merge) return e;
-  return launch_shares_merge(a, D, 4096 / D, stream);
 }
 
 hipError_t launch_paged_stream(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
-  const StreamPlan pl = plan_stream(p, a.kb != nullptr);
-  a.workers = pl.workers; a.min_tiles = pl.min_tiles;
-  a.ws_o = (float*)workspace;
-  a.ws_ml = a.ws_o ? a.ws_o + (size_t)pl.workers * 2 * a.R * p.D : nullptr;
-  return p.D == 128 ? launch_stream<128>(a, pl, stream) : launch_stream<64>(a, pl, stream);
+  set_shares(a, plan_stream(p, a.kb != nullptr), a.R, 1, p.D, workspace);
+  if (p.D == 128) launch_stream<128>(a, stream);
+  else launch_stream<64>(a, stream);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.min_tiles == 0) return e;
+  return launch_shares_merge(a, p.dtype, p.D, 4096 / p.D, stream);
 }
 
 }  // namespace sdllm

@@ -49,13 +49,14 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) sacc[rb][kb] = f32x4{w.neg_m[rb], w.neg_m[rb], w.neg_m[rb], w.neg_m[rb]};
-  // all operand reads first, so that the products find theirs in registers one after the other
+  // all operand reads first, so that the products find theirs in registers one after the other (memory operations stay on their side
+  // of these barriers, arithmetic need not)
   bf16x8 kop[4][NS];
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
     for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
-  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_sched_barrier(0x40f);
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
@@ -66,7 +67,7 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   s16x8 vop[2][NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) vop[0][db] = read_vt(db, 0);
-  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_sched_barrier(0x40f);
   if (missing || above || below) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) hide<4>(sacc[rb], k0, w.pos[rb] - h.window + 1, w.pos[rb] + 1, h.sinks, vis, missing, above, below);
@@ -131,7 +132,7 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   // ---- O^T += V^T P^T
 #pragma unroll
   for (int db = 0; db < NDB; ++db) vop[1][db] = read_vt(db, 1);
-  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_sched_barrier(0x40f);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -160,7 +161,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const Args a = arguments();
     if constexpr (FLAT) {
       if (a->min_tiles == 0) {                     // a workgroup per (sequence, K/V head)
-        open_unit<kTK>(nxt, blockIdx.x / a->Hkv, blockIdx.x % a->Hkv, 0);
+        const int e = divide(blockIdx.x, a->by_Hkv);
+        open_unit<kTK>(nxt, e, blockIdx.x - e * a->Hkv, 0);
         left = nxt.T;
       } else {
         left = open_share<kTK>(blockIdx.x, nxt);
@@ -172,11 +174,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const int v = at / list * kNumXCDs + xcd, unit = v / a->cuts, rank = (at % list) * a->cuts + v % a->cuts;
       if (unit >= a->B * a->Hkv * a->parts || rank >= a->row_tiles) return;
       const int bh = unit / a->parts, part = unit - bh * a->parts;
-      nxt.b = bh / a->Hkv; nxt.kvh = bh - nxt.b * a->Hkv;
-      row_base = (a->row_tiles - 1 - rank) * (WROWS * NW);
-      const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
-      nxt.s = seen_by(a, lens[nxt.b], a->q_lens ? q_lens[nxt.b] : a->K, row_base / a->g, (row_base + WROWS * NW - 1) / a->g, kTK);
-      nxt.T = row_base < nxt.s.q_len * a->g ? max(nxt.s.tiles, 1) : 0;
+      const int b = divide(bh, a->by_Hkv);
+      open_unit<kTK>(nxt, b * a->row_tiles + a->row_tiles - 1 - rank, bh - b * a->Hkv, 0);
+      row_base = nxt.rt * a->tile_rows;
       const int per = max((nxt.T + a->parts - 1) / a->parts, a->min_tiles);
       nxt.i = part * per;
       left = min(per, nxt.T - nxt.i);
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const int g = a->g, last_row = cur.s.q_len * g - 1;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const int R = min(wave_row + 16 * rb + l16, last_row), r = R / g, hq = cur.kvh * g + R - r * g;
+        const int R = min(wave_row + 16 * rb + l16, last_row), r = divide(R, a->by_g), hq = cur.kvh * g + R - r * g;
         const uint16_t* qp = (const uint16_t*)a->q + cur.b * a->q_st[0] + hq * a->q_st[1] + r * a->q_st[2];
 #pragma unroll
         for (int s2 = 0; s2 < NS; ++s2) w.q[rb][s2] = *reinterpret_cast<const bf16x8*>(qp + 32 * s2 + 8 * G);
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int db = 0; db < NDB; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      const int r0 = min(wave_row, last_row) / g, r1 = min(wave_row + WROWS - 1, last_row) / g;
+      const int r0 = divide(min(wave_row, last_row), a->by_g), r1 = divide(min(wave_row + WROWS - 1, last_row), a->by_g);
       const int p0 = cur.s.N - cur.s.q_len;
       all_hi = a->causal ? p0 + r0 + 1 : 0x7fffffff;
       all_lo = a->window > 0 ? p0 + r1 - a->window + 1 : 0;
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       if (R > last_row) continue;
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const int r = R / g, hq = cur.kvh * g + R - r * g;
+        const int r = divide(R, a->by_g), hq = cur.kvh * g + R - r * g;
         uint16_t* orow = (uint16_t*)a->out + cur.b * a->o_st[0] + hq * a->o_st[1] + r * a->o_st[2];
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (G == 0) { a->ws_ml[2 * (slot0 + R)] = w.thr[rb] == kNegBig ? kNegBig : -w.neg_m[rb]; a->ws_ml[2 * (slot0 + R) + 1] = l; }
       }
     }
-    if (redo) redo_rows<D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, slot0);
+    if (redo) redo_rows<uint16_t, D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, slot0);
     if (FLAT) {
       slot = 2LL * blockIdx.x + 1;                 // the first unit's partial result goes to slot 0, the last's to 1
       if (left > 0) { cur.i = cur.T - 1; next_tile<kTK>(cur); }
@@ -375,9 +375,9 @@ __global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int r
   constexpr int TPR = D / 4, RPB = 256 / TPR;
   const long long at = (long long)blockIdx.x * RPB + threadIdx.x / TPR;
   if (at >= (long long)a->B * a->Hkv * a->R) return;
-  const int bh = (int)(at / a->R), R = (int)(at - (long long)bh * a->R), b = bh / a->Hkv, kvh = bh - b * a->Hkv;
+  const int bh = (int)(at / a->R), R = (int)(at - (long long)bh * a->R), b = divide(bh, a->by_Hkv), kvh = bh - b * a->Hkv;
   const int base = R / rows_wg * rows_wg;
-  const Seen s = seen_by(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, base / a->g, (base + rows_wg - 1) / a->g, kTK);
+  const Seen s = seen_by(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, divide(base, a->by_g), divide(base + rows_wg - 1, a->by_g), kTK);
   if (R >= s.q_len * a->g) return;
   const int T = max(s.tiles, 1), per = max((T + a->parts - 1) / a->parts, a->min_tiles), n = (T + per - 1) / per;
   if (n == 1) return;                              // written by its workgroup
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int r
     M = up;
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int r = R / a->g, h = kvh * a->g + R - r * a->g;
+  const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
   uint2 w2;
   w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
   w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
@@ -402,43 +402,28 @@ __global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int r
 }
 
 // ---- launch plan, from the parameters alone
-struct TilePlan { int rb, waves, flat, workers, parts, row_tiles, cuts, min_tiles; };
+struct TilePlan { int rb, waves, flat, parts, row_tiles, cuts, min_tiles; SharePlan shares; };
 
 static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   const long long R = (long long)p.Hq / p.Hkv * p.K, units = (long long)p.B * p.Hkv;
-  const long long N = p.max_kv_len + (with_block ? p.K : 0);
   TilePlan pl{};
   pl.waves = R > 128 ? 8 : 4;
   pl.rb = R > 64 ? 2 : 1;
-  const int rows = 16 * pl.rb * pl.waves;
+  const int rows = 16 * pl.rb * pl.waves, at_once = (pl.waves == 8 ? 1 : 2) * kNumCUs;
   pl.row_tiles = (int)((R + rows - 1) / rows);
   pl.flat = pl.row_tiles == 1 && p.B <= 1024;
-  long long tiles = (N + kTK - 1) / kTK;
-  if (p.window > 0) {
-    const long long span = (rows + p.Hq / p.Hkv - 1) / (p.Hq / p.Hkv);
-    const long long seen = (p.window + (span < p.K ? span : p.K) + kTK - 2) / kTK + 1 + (p.sinks + kTK - 1) / kTK;
-    if (seen < tiles) tiles = seen;
-  }
-  if (tiles < 1) tiles = 1;
-  const long long at_once = (pl.waves == 8 ? 1 : 2) * kNumCUs;
-  pl.min_tiles = 2;
-  if (p.kv_splits > 0) pl.min_tiles = (int)((tiles + p.kv_splits - 1) / p.kv_splits);
+  pl.parts = pl.cuts = 1;
   if (pl.flat) {
-    pl.parts = 1;
-    if (p.kv_splits == 1 || (p.kv_splits == 0 && (units >= 4 * at_once || tiles <= pl.min_tiles))) {
-      pl.workers = (int)units; pl.min_tiles = 0;
-      return pl;
-    }
-    const long long w = (units * tiles + pl.min_tiles - 1) / pl.min_tiles;
-    pl.workers = (int)(p.kv_splits > 0 ? (w < (1 << 20) ? w : 1 << 20) : (w < at_once ? w : at_once));
+    pl.shares = plan_shares(p, with_block, (int)R, 1, kTK, at_once, 2);
     return pl;
   }
+  const long long tiles = paged_most_tiles(p, with_block, rows, kTK);
+  pl.min_tiles = p.kv_splits > 0 ? (int)((tiles + p.kv_splits - 1) / p.kv_splits) : 2;
   long long parts = p.kv_splits > 0 ? p.kv_splits : at_once / (units * pl.row_tiles);
   const long long most = (tiles + pl.min_tiles - 1) / pl.min_tiles;
   if (parts > most) parts = most;
   if (parts < 1) parts = 1;
   pl.parts = (int)parts;
-  pl.cuts = 1;
   while (pl.cuts < kNumXCDs && (p.Hkv * parts * pl.cuts) % kNumXCDs != 0) pl.cuts *= 2;
   return pl;
 }
@@ -446,7 +431,7 @@ static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
 size_t paged_tile_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
   const TilePlan pl = plan_tile(p, with_block);
   const size_t R = (size_t)(p.Hq / p.Hkv) * p.K;
-  if (pl.flat) return pl.min_tiles == 0 ? 0 : (size_t)pl.workers * 2 * R * (p.D + 2) * sizeof(float);
+  if (pl.flat) return share_bytes(pl.shares, (int)R, p.D);
   return pl.parts == 1 ? 0 : (size_t)p.B * p.Hkv * pl.parts * R * (p.D + 2) * sizeof(float);
 }
 
@@ -481,18 +466,25 @@ hipError_t prepare_paged_tile() {
 
 hipError_t launch_paged_tile(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
   const TilePlan pl = plan_tile(p, a.kb != nullptr);
-  a.workers = pl.workers; a.min_tiles = pl.min_tiles; a.parts = pl.parts; a.row_tiles = pl.row_tiles; a.cuts = pl.cuts;
-  const bool merge = pl.flat ? pl.min_tiles > 0 : pl.parts > 1;
-  const size_t slots = pl.flat ? (size_t)pl.workers * 2 : (size_t)p.B * p.Hkv * pl.parts;
-  a.ws_o = merge ? (float*)workspace : nullptr;
-  a.ws_ml = merge ? a.ws_o + slots * a.R * p.D : nullptr;
-  long long grid = pl.workers;
-  if (!pl.flat)
-    grid = ((long long)p.B * p.Hkv * pl.parts * pl.cuts + kNumXCDs - 1) / kNumXCDs * kNumXCDs * ((pl.row_tiles + pl.cuts - 1) / pl.cuts);
+  const int rows_wg = 16 * pl.rb * pl.waves;
+  long long grid;
+  bool merge;
+  if (pl.flat) {
+    set_shares(a, pl.shares, a.R, 1, p.D, workspace);
+    grid = pl.shares.workers;
+    merge = pl.shares.min_tiles > 0;
+  } else {
+    const size_t slots = (size_t)p.B * p.Hkv * pl.parts;
+    a.tile_rows = rows_wg; a.row_tiles = pl.row_tiles; a.by_row_tiles = FastDiv(pl.row_tiles); a.parts = pl.parts; a.cuts = pl.cuts; a.min_tiles = pl.min_tiles;
+    merge = pl.parts > 1;
+    a.ws_o = merge ? (float*)workspace : nullptr;
+    a.ws_ml = merge ? a.ws_o + slots * a.R * p.D : nullptr;
+    grid = ((long long)slots * pl.cuts + kNumXCDs - 1) / kNumXCDs * kNumXCDs * ((pl.row_tiles + pl.cuts - 1) / pl.cuts);
+  }
   hipError_t e = p.D == 128 ? launch_tile_d<128>(a, pl, (unsigned)grid, stream) : launch_tile_d<64>(a, pl, (unsigned)grid, stream);
   if (e != hipSuccess || !merge) return e;
-  if (pl.flat) return launch_shares_merge(a, p.D, kTK, stream);
-  const int rows_wg = 16 * pl.rb * pl.waves, rpb = 256 / (p.D / 4);
+  if (pl.flat) return launch_shares_merge(a, p.dtype, p.D, kTK, stream);
+  const int rpb = 256 / (p.D / 4);
   const unsigned blocks = (unsigned)(((long long)a.B * a.Hkv * a.R + rpb - 1) / rpb);
   if (p.D == 128) hipLaunchKernelGGL(paged_parts_merge_kernel<128>, dim3(blocks), dim3(256), 0, stream, a, rows_wg);
   else hipLaunchKernelGGL(paged_parts_merge_kernel<64>, dim3(blocks), dim3(256), 0, stream, a, rows_wg);
