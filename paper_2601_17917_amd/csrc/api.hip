@@ -181,6 +181,8 @@ int sdllm_init(void) {
   if (e == hipSuccess) e = sdllm::prepare_attention_f32();
   if (e == hipSuccess) e = sdllm::prepare_lm_head();
   if (e == hipSuccess) e = sdllm::prepare_paged_tile();
+  if (e == hipSuccess) e = sdllm::prepare_paged_stream();
+  if (e == hipSuccess) e = sdllm::prepare_paged_f32();
   void* ptr = nullptr;
   if (e == hipSuccess) e = scratch_of_current_device(&ptr);
   if (e != hipSuccess) return fail(SDLLM_ERR_HIP, "init: %s", hipGetErrorString(e));

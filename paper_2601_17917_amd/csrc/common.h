@@ -32,6 +32,8 @@ hipError_t prepare_attention_bf16();   // every opt-in of the module, for the cu
 hipError_t prepare_attention_f32();
 hipError_t prepare_lm_head();
 hipError_t prepare_paged_tile();
+hipError_t prepare_paged_stream();
+hipError_t prepare_paged_f32();
 
 // ---- attention launch plan (host, pure function of the parameters) ----
 struct AttnPlan {

@@ -108,27 +108,30 @@ __device__ __forceinline__ int tiles_to_do(Args a, const Seen& s, int rt) {
   // rows that see nothing are a tile of their own: they are zero
   return rt * a->tile_rows < s.q_len * a->g ? max(s.tiles, 1) : 0;
 }
-// Key tiles of each entry.  The lanes take 64 entries at a time.
-template <int TK>
-__device__ __forceinline__ int tiles_of(Args a, int e) {
-  if (e >= a->B * a->row_tiles) return 0;
-  const int b = divide(e, a->by_row_tiles), rt = e - b * a->row_tiles;
-  return tiles_to_do(a, entry_seen<TK>(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, rt), rt);
+// Key tiles of entries e0 .. e0 + 63, one per lane, and their sums up to the lane
+struct Entries { int n, q_len, tiles, upto; };
+__device__ __forceinline__ int wave_scan(int v) {  // all lanes active
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8: sums within 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15, 31: and over them
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
 }
-__device__ __forceinline__ int wave_scan(int v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int up = __shfl_up(v, d);
-    if ((int)(threadIdx.x & 63) >= d) v += up;
+template <int TK>
+__device__ __forceinline__ Entries entries(Args a, int e0) {
+  Entries x{0, 0, 0, 0};
+  const int e = e0 + (int)(threadIdx.x & 63);
+  if (e < a->B * a->row_tiles) {
+    const int b = divide(e, a->by_row_tiles), rt = e - b * a->row_tiles;
+    x.n = a->lens[b];
+    x.q_len = a->q_lens ? a->q_lens[b] : a->K;
+    x.tiles = tiles_to_do(a, entry_seen<TK>(a, x.n, x.q_len, rt), rt);
   }
-  return v;
+  x.upto = wave_scan(x.tiles);
+  return x;
 }
-template <int TK>
-__device__ __forceinline__ long long all_tiles(Args a) {
-  long long total = 0;
-  for (int e0 = 0; e0 < a->B * a->row_tiles; e0 += 64) total += uniform(__shfl(wave_scan(tiles_of<TK>(a, e0 + (int)(threadIdx.x & 63))), 63));
-  return total * a->Hkv;
-}
+__device__ __forceinline__ int read_lane(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 __device__ __forceinline__ long long tiles_per_worker(Args a, long long total) {
   const long long n = quotient(total + a->workers - 1, a->workers);
   return n > a->min_tiles ? n : a->min_tiles;
@@ -141,36 +144,45 @@ struct Unit {
 };
 
 template <int TK>
-__device__ __forceinline__ void open_unit(Unit& u, int e, int kvh, int i) {
+__device__ __forceinline__ void open_unit(Unit& u, int e, int kvh, int i, int n, int q_len) {
   const Args a = arguments();
   u.e = e; u.b = divide(e, a->by_row_tiles); u.rt = e - u.b * a->row_tiles; u.kvh = kvh; u.i = i;
-  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
-  u.s = entry_seen<TK>(a, lens[u.b], a->q_lens ? q_lens[u.b] : a->K, u.rt);
+  u.s = entry_seen<TK>(a, n, q_len, u.rt);
   u.T = tiles_to_do(a, u.s, u.rt);
+}
+template <int TK>
+__device__ __forceinline__ void open_unit(Unit& u, int e, int kvh, int i) {
+  const Args a = arguments();
+  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
+  const int b = divide(e, a->by_row_tiles);
+  open_unit<TK>(u, e, kvh, i, lens[b], a->q_lens ? q_lens[b] : a->K);
 }
 
 // The unit and tile that the share of worker w begins with; returns the tiles of the share (0: none)
 template <int TK>
 __device__ __forceinline__ int open_share(int w, Unit& u) {
   const Args a = arguments();
-  const int lane = threadIdx.x & 63;
-  const long long total = all_tiles<TK>(a), per = tiles_per_worker(a, total), f = w * per;
+  const int E = a->B * a->row_tiles;
+  Entries x = entries<TK>(a, 0);
+  int chunk = read_lane(x.upto, 63);
+  long long total = chunk;
+  for (int e0 = 64; e0 < E; e0 += 64) total += read_lane(entries<TK>(a, e0).upto, 63);
+  total *= a->Hkv;
+  const long long per = tiles_per_worker(a, total), f = w * per;
   if (f >= total) return 0;
-  long long before = 0;
-  for (int e0 = 0; e0 < a->B * a->row_tiles; e0 += 64) {
-    const int t = tiles_of<TK>(a, e0 + lane), upto = wave_scan(t);
-    const int chunk = uniform(__shfl(upto, 63));
-    if (f < before + (long long)chunk * a->Hkv) {
-      const unsigned long long above = __ballot((long long)upto * a->Hkv > f - before);
-      const int l = __builtin_ctzll(above);
-      const int te = uniform(__shfl(t, l)), first = uniform(__shfl(upto, l)) - te;
-      const long long rest = f - before - (long long)first * a->Hkv;
-      const int kvh = (int)quotient(rest, te);
-      open_unit<TK>(u, e0 + l, kvh, (int)(rest - (long long)kvh * te));
-      break;
-    }
-    before += (long long)chunk * a->Hkv;
+  long long rest = f;                              // tiles in front of it, from entry e0 on
+  int e0 = 0;
+  while (rest >= (long long)chunk * a->Hkv) {
+    rest -= (long long)chunk * a->Hkv;
+    e0 += 64;
+    x = entries<TK>(a, e0);
+    chunk = read_lane(x.upto, 63);
   }
+  const int l = __builtin_ctzll(__ballot((long long)x.upto * a->Hkv > rest));
+  const int t = read_lane(x.tiles, l);
+  rest -= (long long)(read_lane(x.upto, l) - t) * a->Hkv;
+  const int kvh = (int)quotient(rest, t);
+  open_unit<TK>(u, e0 + l, kvh, (int)(rest - (long long)kvh * t), read_lane(x.n, l), read_lane(x.q_len, l));
   return (int)(per < total - f ? per : total - f);
 }
 template <int TK>
@@ -372,13 +384,14 @@ __device__ __forceinline__ void put(uint16_t* p, float x) { *p = __builtin_bit_c
 
 // Rows R0 .. R0 + count - 1 of a unit over its tiles [i0, i1), one row after the other: a lane per key, then a lane per column.  Where the
 // result is finite, what the caller has written stands; else it is written again, as a row of the output or as a partial result
-// (slot0: that of row 0).
+// (those of row 0: part_o, part_ml).
 template <typename T, int D, int TK>
 __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0, int i1, int R0, int count, bool whole,
-                                          long long slot0) {
+                                          float* part_o, float* part_ml) {
   const Args a = arguments();
   const int lane = threadIdx.x & 63;
   wait_transfers();                                // what the caller has written is in front of what is written here
+  wait_lds();
 #pragma unroll 1
   for (int R = R0; R < min(R0 + count, s.q_len * a->g); ++R) {
     const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
@@ -436,8 +449,39 @@ __device__ __forceinline__ void redo_rows(const Seen& s, int b, int kvh, int i0,
       for (int u = 0; u < D / 64; ++u) put(out + lane + 64 * u, o[u] / l);
     } else {
 #pragma unroll
-      for (int u = 0; u < D / 64; ++u) a->ws_o[(slot0 + R) * D + lane + 64 * u] = o[u];
-      if (lane == 0) { a->ws_ml[2 * (slot0 + R)] = m; a->ws_ml[2 * (slot0 + R) + 1] = l; }
+      for (int u = 0; u < D / 64; ++u) part_o[(long long)R * D + lane + 64 * u] = o[u];
+      if (lane == 0) { part_ml[2 * R] = m; part_ml[2 * R + 1] = l; }
+    }
+  }
+}
+
+// Output of `rows` query rows (from R0 on) of a unit that the waves of a workgroup walked together: n partial results in LDS, wave_o
+// floats apart (rows of D) and wave_ml floats apart (reference, sum)
+template <typename T, int D, int THREADS>
+__device__ __forceinline__ void merge_waves(const Unit& u, int R0, int rows, int n, const float* o_s, int wave_o, const float* ml_s, int wave_ml) {
+  const Args a = arguments();
+  constexpr int TPR = D / 4;
+  for (int x = threadIdx.x; x < rows * TPR; x += THREADS) {
+    const int row = x / TPR, d = x % TPR * 4, R = R0 + row;
+    if (R >= u.s.q_len * a->g) break;
+    float M = kNegBig, l = 0.f;
+    for (int k = 0; k < n; ++k) M = fmaxf(M, ml_s[k * wave_ml + 2 * row]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < n; ++k) {
+      const float c = exp2_fast((ml_s[k * wave_ml + 2 * row] - M) * a->scale_log2);
+      acc += *reinterpret_cast<const f32x4*>(o_s + k * wave_o + row * D + d) * c;
+      l += ml_s[k * wave_ml + 2 * row + 1] * c;
+    }
+    acc *= l == 0.f ? 0.f : 1.0f / l;
+    const int r = divide(R, a->by_g), h = u.kvh * a->g + R - r * a->g;
+    T* out = (T*)a->out + u.b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2] + d;
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<f32x4*>(out) = acc;
+    } else {
+      uint2 w;
+      w.x = pack_bf16x2(acc[0], acc[1]);
+      w.y = pack_bf16x2(acc[2], acc[3]);
+      *reinterpret_cast<uint2*>(out) = w;
     }
   }
 }

@@ -13,7 +13,7 @@ __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
   constexpr int TPR = D / 4, RPW = 256 / (TPR * GROUPS);
   __shared__ f32x4 o_s[GROUPS > 1 ? GROUPS : 1][TPR];
   __shared__ float m_s[GROUPS], l_s[GROUPS];
-  const int lane = threadIdx.x & 63, grp = threadIdx.x / TPR % GROUPS, d = threadIdx.x % TPR * 4;
+  const int grp = threadIdx.x / TPR % GROUPS, d = threadIdx.x % TPR * 4;
   // the rows of a workgroup: of one (sequence, K/V head, row tile)
   const int per_tile = (a->tile_rows + RPW - 1) / RPW;
   const unsigned tile = blockIdx.x / (unsigned)per_tile;
@@ -23,12 +23,12 @@ __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
   long long total = 0, start = 0;
   int n = 0;
   for (int e0 = 0; e0 < a->B * a->row_tiles; e0 += 64) {
-    const int t = tiles_of<TK>(a, e0 + lane), upto = wave_scan(t);
+    const Entries x = entries<TK>(a, e0);
     if (e >= e0 && e < e0 + 64) {
-      n = uniform(__shfl(t, e - e0));
-      start = (total + uniform(__shfl(upto, e - e0)) - n) * a->Hkv + (long long)kvh * n;
+      n = read_lane(x.tiles, e - e0);
+      start = (total + read_lane(x.upto, e - e0) - n) * a->Hkv + (long long)kvh * n;
     }
-    total += uniform(__shfl(upto, 63));
+    total += read_lane(x.upto, 63);
   }
   total *= a->Hkv;
   if (n == 0) return;

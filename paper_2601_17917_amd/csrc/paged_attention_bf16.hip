@@ -12,6 +12,7 @@
 //   units.
 // A (sequence, head) that one wave walked alone is written at once; of the others every wave leaves (O, m, l), merged in tile order
 // by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
+//   TOGETHER: the eight waves of a workgroup share the tiles of one (sequence, K/V head) and merge through LDS: no second launch.
 #include "paged_attention.h"
 
 namespace sdllm {
@@ -51,28 +52,44 @@ __device__ __forceinline__ unsigned long long issue_tile(const Hot& h, const Uni
   return vis;
 }
 
-template <int D, int RB>
-__global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
+template <int D, int RB, bool TOGETHER>
+__global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(PagedArgs) {
   using S = StreamShape<D>;
   constexpr int TK = S::TK, KB = S::KB, NS = S::NS, NDB = S::NDB, U = TK / 32;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * S::WAVEB];
+  constexpr int NW = TOGETHER ? 8 : 4;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int lane = threadIdx.x & 63, l16 = lane & 15, G = lane >> 4;
   const int wave = uniform(threadIdx.x >> 6);
   unsigned char* lds_wave = lds + wave * S::WAVEB;
 
   // this wave's tiles
-  const int worker = blockIdx.x * 4 + wave;
+  const int worker = TOGETHER ? blockIdx.x : blockIdx.x * NW + wave;
   Unit nxt;
   int left;                                        // tiles of its share still to do
   {
     const Args a = arguments();
     if (worker >= a->workers) return;
-    if (a->min_tiles == 0) {                       // a wave per (sequence, K/V head)
+    if (a->min_tiles == 0) {                       // a wave, or a workgroup, per (sequence, K/V head)
       const int e = divide(worker, a->by_Hkv);
       open_unit<TK>(nxt, e, worker - e * a->Hkv, 0);
       left = nxt.T;
     } else {
       left = open_share<TK>(worker, nxt);
+    }
+  }
+  [[maybe_unused]] int waves = 0;                  // of the workgroup that have tiles
+  if constexpr (TOGETHER) {
+    const int per = (left + NW - 1) / NW;
+    if (left == 0) return;
+    waves = (left + per - 1) / per;
+    nxt.i = wave * per;
+    left = min(per, left - nxt.i);
+    if (left <= 0) {
+      if (waves > 1) {                             // the barrier that the waves with tiles come to
+        __syncthreads();
+        merge_waves<uint16_t, D, 64 * NW>(nxt, 0, 16 * RB, waves, (const float*)lds, S::WAVEB / 4, (const float*)(lds + NW * S::WAVEB), 32 * RB);
+      }
+      return;
     }
   }
   if (left == 0) return;
@@ -142,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
       wait_lds();
       if (left > 1) {
         next_tile<TK>(nxt);
-        if (nxt.b != cur.b) pages.open(nxt.b);
+        if (!TOGETHER && nxt.b != cur.b) pages.open(nxt.b);
         vis_next = issue_tile<D>(h, nxt, pages, base, lds_wave);
       }
       if (vis == 0) continue;
@@ -244,6 +261,8 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
     const bool whole = begin == 0 && i == cur.T;
     const int g = a->g, last_row = cur.s.q_len * g - 1;
     const long long slot0 = ((long long)worker * 2 + part) * a->R;
+    float* const part_o = TOGETHER ? (float*)lds_wave : a->ws_o + slot0 * D;
+    float* const part_ml = TOGETHER ? (float*)(lds + NW * S::WAVEB) + wave * 32 * RB : a->ws_ml + 2 * slot0;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int R = 16 * rb + l16;
@@ -261,19 +280,36 @@ __global__ __launch_bounds__(256, 2) void paged_stream_kernel(PagedArgs) {
         }
       } else {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(a->ws_o + (slot0 + R) * D + 16 * db + 4 * G) = o[rb][db];
-        if (G == 0) { a->ws_ml[2 * (slot0 + R)] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; a->ws_ml[2 * (slot0 + R) + 1] = lsum[rb]; }
+        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4*>(part_o + R * D + 16 * db + 4 * G) = o[rb][db];
+        if (G == 0) { part_ml[2 * R] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; part_ml[2 * R + 1] = lsum[rb]; }
       }
     }
-    if (redo) redo_rows<uint16_t, D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, slot0);
+    if (redo) redo_rows<uint16_t, D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, part_o, part_ml);
+    if constexpr (TOGETHER) {
+      if (waves > 1) {
+        __syncthreads();
+        merge_waves<uint16_t, D, 64 * NW>(cur, 0, 16 * RB, waves, (const float*)lds, S::WAVEB / 4, (const float*)(lds + NW * S::WAVEB), 32 * RB);
+      }
+      return;
+    }
     part = 1;
   }
 }
 
 static constexpr int kStreamWaves = 8 * kNumCUs;   // resident at once: two workgroups of 64 KiB per CU
 static constexpr int kStreamMinTiles = 2;
+// Waves of a workgroup together, or each for itself (us, 32 query and 8 K/V heads of 128, one row each; together / for itself):
+//   up to 4 units per CU: few keys, where a second launch for the merge costs more than idle CUs do, or no fewer workgroups busy:
+//     1 sequence of 128 keys 5.2 / 10.3, of 1024 11.7 / 11.9, of 2048 21 / 12; 32 of 1024 24 / 30
+//   more: many keys, where a workgroup's start is a small part of its time: 128 sequences of 100 to 4000 keys 185 / 194, 512 of 50 to
+//     1000 182 / 195, 512 of 50 to 200 85 / 48
+static bool together(const sdllm_paged_attn_params& p, bool with_block) {
+  const long long tiles = paged_most_tiles(p, with_block, (long long)p.Hq / p.Hkv * p.K, 4096 / p.D);
+  return p.kv_splits == 0 && ((long long)p.B * p.Hkv < 4 * kNumCUs ? tiles <= 32 : tiles >= 24);
+}
 
 static SharePlan plan_stream(const sdllm_paged_attn_params& p, bool with_block) {
+  if (together(p, with_block)) return SharePlan{p.B * p.Hkv, 0};
   return plan_shares(p, with_block, p.Hq / p.Hkv * p.K, 1, 4096 / p.D, kStreamWaves, kStreamMinTiles);
 }
 
@@ -281,20 +317,30 @@ size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_
   return share_bytes(plan_stream(p, with_block), p.Hq / p.Hkv * p.K, p.D);
 }
 
-template <int D>
-static void launch_stream(const PagedArgs& a, hipStream_t stream) {
-  const dim3 grid((a.workers + 3) / 4);
-  if (a.R <= 16) hipLaunchKernelGGL((paged_stream_kernel<D, 1>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((paged_stream_kernel<D, 2>), grid, dim3(256), 0, stream, a);
+template <int D, int RB>
+static void launch_stream(const PagedArgs& a, bool one_unit, hipStream_t stream) {
+  constexpr int wave_bytes = StreamShape<D>::WAVEB;
+  if (one_unit) hipLaunchKernelGGL((paged_stream_kernel<D, RB, true>), dim3(a.workers), dim3(512), 8 * (wave_bytes + 128 * RB), stream, a);
+  else hipLaunchKernelGGL((paged_stream_kernel<D, RB, false>), dim3((a.workers + 3) / 4), dim3(256), 4 * wave_bytes, stream, a);
 }
 
 hipError_t launch_paged_stream(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
+  const bool one_unit = together(p, a.kb != nullptr);
   set_shares(a, plan_stream(p, a.kb != nullptr), a.R, 1, p.D, workspace);
-  if (p.D == 128) launch_stream<128>(a, stream);
-  else launch_stream<64>(a, stream);
+  if (p.D == 128) a.R <= 16 ? launch_stream<128, 1>(a, one_unit, stream) : launch_stream<128, 2>(a, one_unit, stream);
+  else a.R <= 16 ? launch_stream<64, 1>(a, one_unit, stream) : launch_stream<64, 2>(a, one_unit, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.min_tiles == 0) return e;
   return launch_shares_merge(a, p.dtype, p.D, 4096 / p.D, stream);
+}
+
+// Workgroups of more than 64 KiB of LDS have to be allowed once per device, outside any graph capture
+hipError_t prepare_paged_stream() {
+  const void* kernels[] = {(const void*)paged_stream_kernel<128, 1, true>, (const void*)paged_stream_kernel<128, 2, true>,
+                           (const void*)paged_stream_kernel<64, 1, true>, (const void*)paged_stream_kernel<64, 2, true>};
+  for (const void* k : kernels)
+    if (hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (16384 + 256)); e != hipSuccess) return e;
+  return hipSuccess;
 }
 
 }  // namespace sdllm

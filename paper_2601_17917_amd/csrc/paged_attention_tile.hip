@@ -360,7 +360,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (G == 0) { a->ws_ml[2 * (slot0 + R)] = w.thr[rb] == kNegBig ? kNegBig : -w.neg_m[rb]; a->ws_ml[2 * (slot0 + R) + 1] = l; }
       }
     }
-    if (redo) redo_rows<uint16_t, D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, slot0);
+    if (redo) redo_rows<uint16_t, D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, a->ws_o + slot0 * D, a->ws_ml + 2 * slot0);
     if (FLAT) {
       slot = 2LL * blockIdx.x + 1;                 // the first unit's partial result goes to slot 0, the last's to 1
       if (left > 0) { cur.i = cur.T - 1; next_tile<kTK>(cur); }
