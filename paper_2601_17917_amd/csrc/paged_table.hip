@@ -15,6 +15,7 @@ struct ExtendArgs {
   int B, K, shift, max_pages, n_pages;
 };
 
+constexpr int kReleaseLoads = 8;              // table entries that a lane has in flight
 constexpr int kExtendOneLaunch = 16384;       // rows of the batch up to which the scanning workgroup fills them itself
 
 // Inclusive sum over the workgroup of one value per thread; `total` receives the sum of all.  NT threads, 64-wide waves.
@@ -67,15 +68,26 @@ __global__ __launch_bounds__(NT) void paged_extend_scan_kernel(ExtendArgs a) {
     for (int b0 = 0; b0 < a.B; b0 += NT) {
       const int b = b0 + tid;
       int n = 0;
-      if (b < a.B && a.release[b] != 0) n = (min(max(a.lens[b], 0), cap) + mask) >> a.shift;
+      if (b < a.B) {
+        const int len = a.lens[b];                 // asked for at once with the flag
+        n = a.release[b] != 0 ? (min(max(len, 0), cap) + mask) >> a.shift : 0;
+      }
       int total;
       const int upto = block_scan<NT>(n, wave_sums, total);
       __syncthreads();                         // the previous chunk's entries are read
       s_first[tid] = avail + upto - n; s_n[tid] = n;
       __syncthreads();
       for (int i = tid >> 6; i < min(NT, a.B - b0); i += NT / 64)       // a wave per sequence
-        for (int e = tid & 63; e < s_n[i]; e += 64)
-          if (s_first[i] + e < a.n_pages) a.free_pages[s_first[i] + e] = a.table[(long long)(b0 + i) * a.max_pages + e];
+        for (int e0 = tid & 63; e0 < s_n[i]; e0 += 64 * kReleaseLoads) {
+          const int32_t* row = a.table + (long long)(b0 + i) * a.max_pages;
+          const int first = s_first[i], n = min(s_n[i], a.n_pages - first);
+          int page[kReleaseLoads];
+#pragma unroll
+          for (int u = 0; u < kReleaseLoads; ++u) page[u] = row[min(e0 + 64 * u, s_n[i] - 1)];
+#pragma unroll
+          for (int u = 0; u < kReleaseLoads; ++u)
+            if (e0 + 64 * u < n) a.free_pages[first + e0 + 64 * u] = page[u];
+        }
       avail = min(avail + total, a.n_pages);
     }
     __syncthreads();                           // pushed entries may be popped below

@@ -7,7 +7,8 @@
 // turns, position * f_i / 2 pi, in double (its fraction is what counts, and float loses it beyond a few thousand positions), the
 // fraction's sine and cosine in float.  A lane holds two 16-byte vectors of a row that contain whole pairs -- (i, i + R/2) as a
 // vector of the first half and the matching one of the second, or adjacent vectors -- so that the rotation needs no exchange
-// between lanes; the sum of squares is reduced over the 4 to 32 lanes of a row.
+// between lanes; the sum of squares is reduced over the 4 to 32 lanes of a row.  Several tokens for a workgroup were slower (36 to 42
+// us for 2 x 4096 tokens of 36 heads of 128, 4.9 TB/s and 31 us this way).
 #include "paged_common.h"
 #include <cmath>
 
@@ -51,7 +52,7 @@ template <> struct Vec<uint16_t> {                           // bf16 bit pattern
 };
 
 // GL lanes per row (a power of two, at least D / (2 N); the lanes beyond idle)
-template <typename T, int GL, bool INTERLEAVED>
+template <typename T, int GL, bool INTERLEAVED, bool STREAMING>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
   constexpr int N = Vec<T>::N;
   __shared__ float cos_s[kMaxPairs], sin_s[kMaxPairs];
@@ -69,6 +70,18 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
   else { va = j; vb = j + half; }
   const int first = INTERLEAVED ? j * N : va * N;            // its first pair
 
+  const int row0 = blockIdx.y * a.rows_per_chunk, row1 = min(row0 + a.rows_per_chunk, a.rows);
+  u32x4 na{}, nb{};                                // a row's loads travel under the angles, or under the row before
+  auto load = [&](int row) {
+    if (row >= row1 || !active) return;
+    const bool is_q = row < a.Hq, is_v = row >= a.Hq + a.Hkv;
+    const int h = is_q ? row : (is_v ? row - a.Hq - a.Hkv : row - a.Hq);
+    const long long* st = is_q ? a.q_st : (is_v ? a.v_st : a.k_st);
+    const T* src = (const T*)(is_q ? a.q : (is_v ? a.v : a.k)) + b * st[0] + h * st[1] + t * st[2];
+    na = *reinterpret_cast<const u32x4*>(src + va * N);
+    nb = *reinterpret_cast<const u32x4*>(src + vb * N);
+  };
+  load(row0 + tid / GL);
   for (int i = tid; i < a.R / 2; i += 256) {
     const int pos = a.per_row ? a.positions[token] : a.positions[b] + t;
     const double x = (double)pos * a.turns[i];
@@ -80,13 +93,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
   const int slot = a.slots != nullptr ? a.slots[token] : -1;
   __syncthreads();
 
-  const int row0 = blockIdx.y * a.rows_per_chunk, row1 = min(row0 + a.rows_per_chunk, a.rows);
   for (int row = row0 + tid / GL; row < row1; row += 256 / GL) {
     // which tensor: uniform over the lanes of a row
     const bool is_q = row < a.Hq, is_v = row >= a.Hq + a.Hkv;
     const int h = is_q ? row : (is_v ? row - a.Hq - a.Hkv : row - a.Hq);
-    const long long* st = is_q ? a.q_st : (is_v ? a.v_st : a.k_st);
-    const T* src = (const T*)(is_q ? a.q : (is_v ? a.v : a.k)) + b * st[0] + h * st[1] + t * st[2];
+    const u32x4 ra = na, rb = nb;
+    load(row + 256 / GL);
     T* dst;
     if (is_q) dst = (T*)a.q_out + b * a.qo_st[0] + h * a.qo_st[1] + t * a.qo_st[2];
     else if (a.slots == nullptr) dst = (T*)a.k_out + b * a.ko_st[0] + h * a.ko_st[1] + t * a.ko_st[2];
@@ -95,13 +107,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
       const int page = slot >> a.shift, r = slot & ((1 << a.shift) - 1);
       dst = (T*)(is_v ? a.v_pages : a.k_pages) + ((((long long)page * a.Hkv + h) << a.shift) + r) * a.D;
     }
-    u32x4 ra{}, rb{};
-    if (active) {
-      ra = *reinterpret_cast<const u32x4*>(src + va * N);
-      rb = *reinterpret_cast<const u32x4*>(src + vb * N);
-    }
+    auto store = [&](const u32x4& x, const u32x4& y) {
+      u32x4 *to = reinterpret_cast<u32x4*>(dst + va * N), *to2 = reinterpret_cast<u32x4*>(dst + vb * N);
+      if constexpr (STREAMING) { __builtin_nontemporal_store(x, to); __builtin_nontemporal_store(y, to2); }
+      else { *to = x; *to2 = y; }
+    };
     if (is_v) {
-      if (active) { *reinterpret_cast<u32x4*>(dst + va * N) = ra; *reinterpret_cast<u32x4*>(dst + vb * N) = rb; }
+      if (active) store(ra, rb);
       continue;
     }
     float x[2 * N];
@@ -135,15 +147,19 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
 #pragma unroll
       for (int e = 0; e < 2 * N; ++e) x[e] = y[e];
     }
-    *reinterpret_cast<u32x4*>(dst + va * N) = Vec<T>::pack(x);
-    *reinterpret_cast<u32x4*>(dst + vb * N) = Vec<T>::pack(x + N);
+    store(Vec<T>::pack(x), Vec<T>::pack(x + N));
   }
 }
 
 template <typename T, int GL>
-static void launch_gl(const NormRopeArgs& a, bool interleaved, dim3 grid, hipStream_t stream) {
-  if (interleaved) hipLaunchKernelGGL((qk_norm_rope_kernel<T, GL, true>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((qk_norm_rope_kernel<T, GL, false>), grid, dim3(256), 0, stream, a);
+static void launch_gl(const NormRopeArgs& a, bool interleaved, bool streaming, dim3 grid, hipStream_t stream) {
+  if (interleaved) {
+    if (streaming) hipLaunchKernelGGL((qk_norm_rope_kernel<T, GL, true, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, GL, true, false>), grid, dim3(256), 0, stream, a);
+  } else {
+    if (streaming) hipLaunchKernelGGL((qk_norm_rope_kernel<T, GL, false, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<T, GL, false, false>), grid, dim3(256), 0, stream, a);
+  }
 }
 
 static void dense_or(const int64_t* given, int H, int K, int D, long long* out) {
@@ -167,6 +183,9 @@ hipError_t launch_qk_norm_rope(const sdllm_qk_norm_rope_params& p, const void* q
   a.K = p.K; a.Hq = p.Hq; a.Hkv = p.Hkv; a.D = p.D; a.R = p.rotary_dim; a.per_row = p.positions_per_row;
   a.shift = slots ? __builtin_ctz(p.page_size) : 0;
   a.slots_total = slots ? p.n_pages << a.shift : 0;
+  // What is more than the L2s hold is not kept there for the reader.  (2 x 4096 tokens of 36 heads of 128: 31.1 us, against 33.0 through
+  // L2; 2 x 4000 of 48 heads of 64: 18.7, 25.3.)
+  const bool streaming = (double)p.B * p.K * (p.Hq + p.Hkv * (slots ? 2 : 1)) * p.D * (p.dtype == SDLLM_FP32 ? 4 : 2) > 32e6;
   a.eps = p.eps; a.amplitude = p.amplitude;
   a.rows = p.Hq + p.Hkv * (slots ? 2 : 1);
   // turns per position of pair i: theta^(-2i/R) / 2 pi, by repeated multiplication (64 roundings of 2^-53)
@@ -193,14 +212,14 @@ hipError_t launch_qk_norm_rope(const sdllm_qk_norm_rope_params& p, const void* q
   const dim3 grid((unsigned)tokens, (unsigned)chunks);
   const bool il = p.interleaved != 0;
   if (f32) {
-    if (gl == 4) launch_gl<float, 4>(a, il, grid, stream);
-    else if (gl == 8) launch_gl<float, 8>(a, il, grid, stream);
-    else if (gl == 16) launch_gl<float, 16>(a, il, grid, stream);
-    else launch_gl<float, 32>(a, il, grid, stream);
+    if (gl == 4) launch_gl<float, 4>(a, il, streaming, grid, stream);
+    else if (gl == 8) launch_gl<float, 8>(a, il, streaming, grid, stream);
+    else if (gl == 16) launch_gl<float, 16>(a, il, streaming, grid, stream);
+    else launch_gl<float, 32>(a, il, streaming, grid, stream);
   } else {
-    if (gl == 4) launch_gl<uint16_t, 4>(a, il, grid, stream);
-    else if (gl == 8) launch_gl<uint16_t, 8>(a, il, grid, stream);
-    else launch_gl<uint16_t, 16>(a, il, grid, stream);
+    if (gl == 4) launch_gl<uint16_t, 4>(a, il, streaming, grid, stream);
+    else if (gl == 8) launch_gl<uint16_t, 8>(a, il, streaming, grid, stream);
+    else launch_gl<uint16_t, 16>(a, il, streaming, grid, stream);
   }
   return hipGetLastError();
 }
