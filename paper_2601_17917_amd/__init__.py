@@ -582,7 +582,7 @@ def _on_current_device(*tensors):
     import torch
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != dev:
+        if t is not None and t.get_device() != dev:
             raise SdllmError(ERR_INVALID_ARG, f"a tensor is on {t.device}, the current device is cuda:{dev}")
 
 
@@ -598,7 +598,7 @@ def _new(shape, dtype, device, stream):
 
 def _shaped(t, name, shape, dtype):
     """A dense device tensor of this shape and type."""
-    if t is None:
+    if t is None or (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.shape == shape):
         return
     _require(t, name, dtype)
     if t.shape != shape:
@@ -615,12 +615,13 @@ def _strides(t, name, shape, dtype):
         raise SdllmError(ERR_INVALID_ARG, f"{name} must be {list(shape)}, is {list(t.shape)}")
     if t.is_contiguous():
         return _Stride(0, 0, 0)
-    st, n = t.stride(), t.shape
-    if st[3] != 1:
+    b, h, k, last = t.stride()
+    nb, nh, nk, _ = shape
+    if last != 1:
         raise SdllmError(ERR_INVALID_ARG, f"{name} must have a contiguous last dimension")
-    if any(st[i] == 0 and n[i] > 1 for i in range(3)):
+    if (b == 0 and nb > 1) or (h == 0 and nh > 1) or (k == 0 and nk > 1):
         raise SdllmError(ERR_INVALID_ARG, f"{name} is a broadcast view")
-    return _Stride(*(st[i] if n[i] > 1 else 0 for i in range(3)))     # the stride of a dimension of one row says nothing
+    return _Stride(b if nb > 1 else 0, h if nh > 1 else 0, k if nk > 1 else 0)   # the stride of a dimension of one row says nothing
 
 
 def paged_extend(*args, **kw):

@@ -110,14 +110,6 @@ __device__ __forceinline__ int tiles_to_do(Args a, const Seen& s, int rt) {
 }
 // Key tiles of entries e0 .. e0 + 63, one per lane, and their sums up to the lane
 struct Entries { int n, q_len, tiles, upto; };
-__device__ __forceinline__ int wave_scan(int v) {  // all lanes active
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8: sums within 16 lanes
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15, 31: and over them
-  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-}
 template <int TK>
 __device__ __forceinline__ Entries entries(Args a, int e0) {
   Entries x{0, 0, 0, 0};

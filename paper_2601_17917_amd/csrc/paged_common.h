@@ -20,6 +20,16 @@ struct FastDiv {
   }
 };
 
+// Sum of a value over the lanes up to this one; all lanes active
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8: sums within 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15, 31: and over them
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+}
+
 // Errors of entry points that live outside api.hip end up in the same per-thread text (sdllm_last_error)
 int set_error(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
