@@ -4,8 +4,8 @@
 // A workgroup owns 16 RB NW query rows (NW waves, 16 RB rows each) and walks key tiles of 64 that its waves share through a
 // ring in LDS: each wave moves 16-row slabs global -> LDS, one tile ahead of the one being computed (four waves, two workgroups per CU)
 // or two (eight waves, one workgroup per CU), one barrier per tile.  Products, operand layouts and the softmax are those of the stream kernel.
-//   FLAT: one row tile covers a (sequence, K/V head).  The workgroups walk equal shares of all key tiles of the call, laid end to end
-//         as the stream kernel's waves do, so that lengths need not be alike.
+//   FLAT (four waves of 16 rows): one row tile covers a (sequence, K/V head).  The workgroups walk equal shares of all key tiles of
+//         the call, laid end to end as the stream kernel's waves do, so that lengths need not be alike.
 //   else: a workgroup per (row tile, sequence, K/V head, part of the keys it sees); the tiles of the last rows, which see most under a
 //         causal mask, come first.
 #include "paged_attention.h"
@@ -49,14 +49,14 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) sacc[rb][kb] = f32x4{w.neg_m[rb], w.neg_m[rb], w.neg_m[rb], w.neg_m[rb]};
-  // all operand reads first, so that the products find theirs in registers one after the other (memory operations stay on their side
-  // of these barriers, arithmetic need not)
+  // all operand reads first, so that the products find theirs in registers one after the other (memory operations and products stay on
+  // their side of these barriers, other arithmetic need not)
   bf16x8 kop[4][NS];
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
     for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
-  __builtin_amdgcn_sched_barrier(0x40f);
+  __builtin_amdgcn_sched_barrier(0x406);
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
@@ -67,7 +67,7 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   s16x8 vop[2][NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) vop[0][db] = read_vt(db, 0);
-  __builtin_amdgcn_sched_barrier(0x40f);
+  __builtin_amdgcn_sched_barrier(0x406);
   if (missing || above || below) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) hide<4>(sacc[rb], k0, w.pos[rb] - h.window + 1, w.pos[rb] + 1, h.sinks, vis, missing, above, below);
@@ -132,7 +132,7 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   // ---- O^T += V^T P^T
 #pragma unroll
   for (int db = 0; db < NDB; ++db) vop[1][db] = read_vt(db, 1);
-  __builtin_amdgcn_sched_barrier(0x40f);
+  __builtin_amdgcn_sched_barrier(0x406);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
   // ---- this workgroup's tiles
   Unit nxt;
-  int left, row_base = 0;                          // tiles still to do; first query row
+  int left;                                        // tiles still to do
   long long slot = 2LL * blockIdx.x;               // of its partial results
   {
     const Args a = arguments();
@@ -176,7 +176,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const int bh = unit / a->parts, part = unit - bh * a->parts;
       const int b = divide(bh, a->by_Hkv);
       open_unit<kTK>(nxt, b * a->row_tiles + a->row_tiles - 1 - rank, bh - b * a->Hkv, 0);
-      row_base = nxt.rt * a->tile_rows;
       const int per = max((nxt.T + a->parts - 1) / a->parts, a->min_tiles);
       nxt.i = part * per;
       left = min(per, nxt.T - nxt.i);
@@ -258,13 +257,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   int stage = 0;
   while (left > 0) {
     // ---- a unit
-    const int begin = cur.i, wave_row = row_base + wave * WROWS;
+    const int begin = cur.i;
+    int wave_row;                                  // the wave's first query row
     Rows<D, RB> w;
     int wg_hi, wg_lo;                              // ... of the workgroup's rows
     int all_lo, all_hi;                            // keys that all of the wave's rows see: [all_lo, all_hi) as far as they exist
     {
       const Args a = arguments();
       const int g = a->g, last_row = cur.s.q_len * g - 1;
+      wave_row = cur.rt * a->tile_rows + wave * WROWS;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int R = min(wave_row + 16 * rb + l16, last_row), r = divide(R, a->by_g), hq = cur.kvh * g + R - r * g;
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const Args a = arguments();
     const bool whole = begin == 0 && i == cur.T;
     const int g = a->g, last_row = cur.s.q_len * g - 1;
-    const long long slot0 = slot * a->R;
+    const long long slot0 = FLAT ? (slot - cur.rt) * a->tile_rows : slot * a->R;   // of row 0
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float l = w.lsum[rb];
@@ -402,19 +403,29 @@ __global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int r
 }
 
 // ---- launch plan, from the parameters alone
-struct TilePlan { int rb, waves, flat, parts, row_tiles, cuts, min_tiles; SharePlan shares; };
+// Rows of a workgroup and the sharing of the work by rows R per (sequence, K/V head) (us; lengths 500 to 8000, 8 sequences, heads of
+// 128 unless stated):
+//   up to 64: four waves of 16 rows, equal shares: 32 heads of 64 rows 130, in parts 145; 28 and 4 heads, 16 rows a head (R = 112) 40, in
+//     parts 34
+//   up to 256: four waves of 32 rows, in parts, whose row tiles find K and V in L2: R = 224 40 us, eight waves in shares 47; 32
+//     sequences of 100 to 4000, R = 256, 126 and 168
+//   more: eight waves of 32 rows, so that K and V come from L2 half as often: 2 x 2048 rows of 32 / 8 heads behind 4096 keys 321, four
+//     waves 344; 8 x 512 rows over 4096 keys 257 and 271 (heads of 64: 188 and 190)
+struct TilePlan { int rb, waves, flat, parts, tile_rows, row_tiles, cuts, min_tiles; SharePlan shares; };
 
 static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   const long long R = (long long)p.Hq / p.Hkv * p.K, units = (long long)p.B * p.Hkv;
   TilePlan pl{};
-  pl.waves = R > 128 ? 8 : 4;
+  pl.waves = R > 256 ? 8 : 4;
   pl.rb = R > 64 ? 2 : 1;
   const int rows = 16 * pl.rb * pl.waves, at_once = (pl.waves == 8 ? 1 : 2) * kNumCUs;
   pl.row_tiles = (int)((R + rows - 1) / rows);
-  pl.flat = pl.row_tiles == 1 && p.B <= 1024;
+  pl.tile_rows = rows;
+  pl.flat = R <= 64;
   pl.parts = pl.cuts = 1;
   if (pl.flat) {
-    pl.shares = plan_shares(p, with_block, (int)R, 1, kTK, at_once, 2);
+    pl.tile_rows = (int)R;
+    pl.shares = plan_shares(p, with_block, pl.tile_rows, 1, kTK, at_once, 2);
     return pl;
   }
   const long long tiles = paged_most_tiles(p, with_block, rows, kTK);
@@ -431,7 +442,7 @@ static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
 size_t paged_tile_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
   const TilePlan pl = plan_tile(p, with_block);
   const size_t R = (size_t)(p.Hq / p.Hkv) * p.K;
-  if (pl.flat) return share_bytes(pl.shares, (int)R, p.D);
+  if (pl.flat) return share_bytes(pl.shares, pl.tile_rows, p.D);
   return pl.parts == 1 ? 0 : (size_t)p.B * p.Hkv * pl.parts * R * (p.D + 2) * sizeof(float);
 }
 
@@ -446,21 +457,18 @@ static hipError_t launch_tile(const PagedArgs& a, unsigned grid, hipStream_t str
 }
 template <int D>
 static hipError_t launch_tile_d(const PagedArgs& a, const TilePlan& pl, unsigned grid, hipStream_t stream, bool launch = true) {
-  if (pl.waves == 8) return pl.flat ? launch_tile<D, 2, 8, true>(a, grid, stream, launch) : launch_tile<D, 2, 8, false>(a, grid, stream, launch);
-  if (pl.rb == 2) return pl.flat ? launch_tile<D, 2, 4, true>(a, grid, stream, launch) : launch_tile<D, 2, 4, false>(a, grid, stream, launch);
-  return pl.flat ? launch_tile<D, 1, 4, true>(a, grid, stream, launch) : launch_tile<D, 1, 4, false>(a, grid, stream, launch);
+  if (pl.waves == 8) return launch_tile<D, 2, 8, false>(a, grid, stream, launch);
+  return pl.flat ? launch_tile<D, 1, 4, true>(a, grid, stream, launch) : launch_tile<D, 2, 4, false>(a, grid, stream, launch);
 }
 
 hipError_t prepare_paged_tile() {
   hipError_t e = hipSuccess;
-  for (int waves = 4; waves <= 8; waves += 4)
-    for (int rb = 1; rb <= 2; ++rb)
-      for (int flat = 0; flat <= 1; ++flat) {
-        TilePlan pl{};
-        pl.waves = waves; pl.rb = rb; pl.flat = flat;
-        if (e == hipSuccess) e = launch_tile_d<64>(PagedArgs{}, pl, 0, nullptr, false);
-        if (e == hipSuccess) e = launch_tile_d<128>(PagedArgs{}, pl, 0, nullptr, false);
-      }
+  for (int variant = 0; variant < 3; ++variant) {
+    TilePlan pl{};
+    pl.waves = variant == 2 ? 8 : 4; pl.flat = variant == 0;
+    if (e == hipSuccess) e = launch_tile_d<64>(PagedArgs{}, pl, 0, nullptr, false);
+    if (e == hipSuccess) e = launch_tile_d<128>(PagedArgs{}, pl, 0, nullptr, false);
+  }
   return e;
 }
 
@@ -470,12 +478,12 @@ hipError_t launch_paged_tile(const sdllm_paged_attn_params& p, PagedArgs& a, voi
   long long grid;
   bool merge;
   if (pl.flat) {
-    set_shares(a, pl.shares, a.R, 1, p.D, workspace);
+    set_shares(a, pl.shares, pl.tile_rows, pl.row_tiles, p.D, workspace);
     grid = pl.shares.workers;
     merge = pl.shares.min_tiles > 0;
   } else {
     const size_t slots = (size_t)p.B * p.Hkv * pl.parts;
-    a.tile_rows = rows_wg; a.row_tiles = pl.row_tiles; a.by_row_tiles = FastDiv(pl.row_tiles); a.parts = pl.parts; a.cuts = pl.cuts; a.min_tiles = pl.min_tiles;
+    a.tile_rows = pl.tile_rows; a.row_tiles = pl.row_tiles; a.by_row_tiles = FastDiv(pl.row_tiles); a.parts = pl.parts; a.cuts = pl.cuts; a.min_tiles = pl.min_tiles;
     merge = pl.parts > 1;
     a.ws_o = merge ? (float*)workspace : nullptr;
     a.ws_ml = merge ? a.ws_o + slots * a.R * p.D : nullptr;
