@@ -144,13 +144,15 @@ int sdllm_paged_kv_append(const sdllm_paged_append_params* p,
  * key is zero, and what is stored for hidden keys, or behind the last one in a page, does not matter, NaN included.
  * One token per sequence (K = 1), the rows of a block and the pieces of prompts are the same call.
  *
- *   B, Hq, Hkv, D   as for sdllm_block_attention; D in {64, 128} for both dtypes; B * Hkv < 2^22
+ *   B, Hq, Hkv, D   as for sdllm_block_attention; D in {64, 128} for both dtypes; B * Hkv < 2^22,
+ *                   B * Hq * K < 2^28
  *   K               query rows per sequence of q, out and the block (>= 1)
  *   page_size, n_pages, max_pages (entries of a table row, > 0); a page of all heads below 2 GiB
  *   max_kv_len      upper bound of kv_lens, <= max_pages * page_size: the launch plan is made for it (the lengths themselves are
  *                   device data); max_kv_len + K <= 2^30
  *   scale           softmax scale; <= 0 selects 1/sqrt(D)
- *   kv_splits       0 = choose automatically; n >= 1: a sequence of max_kv_len keys is cut into about n parts
+ *   kv_splits       0 = choose automatically; n >= 1: a sequence of max_kv_len keys is cut into about n parts, if the batch is not so
+ *                   large that parts gain nothing
  *   *_stride        as for sdllm_qk_norm_rope
  * Out of range: kv_lens is clamped to [0, max_kv_len], q_lens to [0, K]; the keys of a page id outside [0, n_pages) are hidden
  * (a page that has left the window may be given back and its entry set to -1).

@@ -124,8 +124,8 @@ int check_paged_attn(const sdllm_paged_attn_params* p, bool with_block) {
   if (p->kv_splits < 0) return set_error(kInvalid, "%s: kv_splits must be >= 0", w);
   if (!(p->scale == p->scale) || std::isinf(p->scale)) return set_error(kInvalid, "%s: scale is not finite", w);
   const long long rows = (long long)p->Hq * p->K;
-  if ((long long)p->max_kv_len + p->K > (1LL << 30) || (long long)p->B * p->Hkv >= (1LL << 22) || rows > 0x7fffffffLL ||
-      rows * p->B > 0x7fffffffLL || (long long)p->B * p->max_pages > 0x7fffffffLL)
+  if ((long long)p->max_kv_len + p->K > (1LL << 30) || (long long)p->B * p->Hkv >= (1LL << 22) || rows >= (1LL << 28) ||
+      rows * p->B >= (1LL << 28) || (long long)p->B * p->max_pages > 0x7fffffffLL)
     return set_error(kUnsupported, "%s: sequence or batch too large", w);
   const int e = p->dtype == SDLLM_FP32 ? 4 : 2;
   if ((long long)p->Hkv * p->page_size * p->D * e >= (1LL << 31)) return set_error(kUnsupported, "%s: a page of all heads must be below 2 GiB", w);

@@ -135,7 +135,7 @@ SharePlan plan_shares(const sdllm_paged_attn_params& p, bool with_block, int til
   const long long per = p.kv_splits > 0 ? (tiles + p.kv_splits - 1) / p.kv_splits : min_tiles;
   // A worker per unit where a unit is one share anyway, where the units go round all workers several times, and where finding the
   // shares (a walk over the batch's lengths) or the merge's grid would get long
-  if (p.kv_splits == 1 || tiles <= per || units * tile_rows >= (1 << 23) || (p.kv_splits == 0 && (units >= 2LL * at_once || (long long)p.B * row_tiles > 2048)))
+  if (p.kv_splits == 1 || tiles <= per || units * tile_rows >= (1 << 23) || (long long)p.B * row_tiles > 2048 || (p.kv_splits == 0 && units >= 2LL * at_once))
     return SharePlan{(int)units, 0};
   const long long w = (units * tiles + per - 1) / per, most = p.kv_splits > 0 ? 1 << 18 : at_once;
   return SharePlan{(int)(w < most ? w : most), (int)per};
@@ -177,7 +177,9 @@ hipError_t launch_paged_attention(const sdllm_paged_attn_params& p, const void* 
   dense_or(p.v_block_stride, p.Hkv, p.K, p.D, a.vb_st);
   a.B = p.B; a.Hq = p.Hq; a.Hkv = p.Hkv; a.g = p.Hq / p.Hkv; a.K = p.K; a.R = a.g * p.K;
   a.shift = __builtin_ctz(p.page_size); a.page_bytes = (unsigned)((long long)p.Hkv * p.page_size * p.D * (p.dtype == SDLLM_FP32 ? 4 : 2));
-  a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.max_kv = p.max_kv_len; a.causal = p.causal; a.window = p.window; a.sinks = p.sinks;
+  a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.max_kv = p.max_kv_len; a.causal = p.causal;
+  // positions lie between -2^30 and 2^30: as far as the differences of two of them stay within 32 bits
+  a.window = p.window < (1 << 30) ? p.window : 1 << 30; a.sinks = p.sinks < (1 << 30) ? p.sinks : 1 << 30;
   a.by_g = FastDiv(a.g); a.by_Hkv = FastDiv(a.Hkv);
   const float scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.D);
   a.scale_log2 = scale * kLog2e; a.thr8 = 8.0f / a.scale_log2;

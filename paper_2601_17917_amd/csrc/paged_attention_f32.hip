@@ -245,7 +245,8 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_f32_kernel(Page
 //     200 157 / 115
 static bool together(const sdllm_paged_attn_params& p, bool with_block, int row_tiles) {
   const long long tiles = paged_most_tiles(p, with_block, 16, 16);
-  return p.kv_splits == 0 && ((long long)p.B * p.Hkv * row_tiles < kNumCUs ? tiles * p.D <= 2560 : tiles >= 32);
+  const long long units = (long long)p.B * p.Hkv * row_tiles;
+  return p.kv_splits == 0 && (units < kNumCUs ? tiles * p.D <= 2560 : tiles >= 32 && units < (1 << 22));   // a launch has fewer than 2^32 threads
 }
 
 static int row_tiles_of(const sdllm_paged_attn_params& p) { return (int)(((long long)p.Hq / p.Hkv * p.K + 15) / 16); }

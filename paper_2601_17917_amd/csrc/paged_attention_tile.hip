@@ -431,7 +431,8 @@ static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   const long long tiles = paged_most_tiles(p, with_block, rows, kTK);
   pl.min_tiles = p.kv_splits > 0 ? (int)((tiles + p.kv_splits - 1) / p.kv_splits) : 2;
   long long parts = p.kv_splits > 0 ? p.kv_splits : at_once / (units * pl.row_tiles);
-  const long long most = (tiles + pl.min_tiles - 1) / pl.min_tiles;
+  long long most = (tiles + pl.min_tiles - 1) / pl.min_tiles;
+  if (most * units * pl.row_tiles > (1 << 20)) most = (1 << 20) / (units * pl.row_tiles);   // workgroups, and what the merge has to read
   if (parts > most) parts = most;
   if (parts < 1) parts = 1;
   pl.parts = (int)parts;
