@@ -13,8 +13,8 @@ struct PagedArgs {
   int shift, n_pages, max_pages, max_kv, causal, window, sinks;
   unsigned page_bytes;                             // of one page, all heads
   int tile_rows, row_tiles;                        // query rows of a unit; units of a (sequence, K/V head)
-  int workers, parts, cuts, min_tiles;             // how the key tiles are shared out (see the kernels)
-  FastDiv by_g, by_row_tiles, by_Hkv;
+  int workers, cuts, min_tiles;                    // how the key tiles are shared out (see the kernels)
+  FastDiv by_g, by_row_tiles, by_Hkv, by_tile_rows;
   float scale_log2, thr8;                          // thr8: 8 in log2 units, as a difference of scores
 };
 

@@ -6,9 +6,11 @@
 // or two (eight waves, one workgroup per CU), one barrier per tile.  Products, operand layouts and the softmax are those of the stream kernel.
 //   FLAT (four waves of 16 rows): one row tile covers a (sequence, K/V head).  The workgroups walk equal shares of all key tiles of
 //         the call, laid end to end as the stream kernel's waves do, so that lengths need not be alike.
-//   else: a workgroup per (row tile, sequence, K/V head, part of the keys it sees); the tiles of the last rows, which see most under a
-//         causal mask, come first.
+//   else: a workgroup per (row tile, sequence, K/V head), the tiles of the last rows, which see most under a causal mask, first; or,
+//         where that is fewer than fit on the chip, per (row tile, sequence, K/V head, part of the keys).  Sequences get parts by their
+//         lengths: parts have as few tiles as let all workgroups be on the chip at once.
 #include "paged_attention.h"
+#include <algorithm>
 
 namespace sdllm {
 
@@ -142,6 +144,48 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
         w.o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop[u][db]), __builtin_bit_cast(bf16x8, pk[rb][u]), w.o[rb][db], 0, 0, 0);
 }
 
+// ---- Parts: u counts (sequence, part, K/V head) over the call.
+// Tiles that decide on the number of parts of sequence b: of its first or its last row tile, whichever has more
+__device__ __forceinline__ int tiles_of_sequence(Args a, int b) {
+  if (b >= a->B) return 0;
+  const int n = a->lens[b], q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
+  if (q_len == 0) return 0;
+  const int last = divide(q_len * a->g - 1, a->by_tile_rows);
+  return max(tiles_to_do(a, entry_seen<kTK>(a, n, q_len, 0), 0), tiles_to_do(a, entry_seen<kTK>(a, n, q_len, last), last));
+}
+struct Part { int b, kvh, index, n; };             // part `index` of n
+// Number u0 of the first of a sequence's parts, for u >= 0 of the sequence that u belongs to, else of sequence p.b; false: none
+__device__ __forceinline__ bool find_part(int u, Part& p, int& u0) {
+  const Args a = arguments();
+  const int lane = threadIdx.x & 63;
+  int t = tiles_of_sequence(a, lane);
+  long long total = read_lane(wave_scan(t), 63);
+  for (int b0 = 64; b0 < a->B; b0 += 64) total += read_lane(wave_scan(tiles_of_sequence(a, b0 + lane)), 63);
+  // Tiles of a part: so many that there are no more parts than workers (one to a K/V head and sequence always fits)
+  int per = (int)tiles_per_worker(a, total * a->Hkv);
+  while (true) {
+    long long n = read_lane(wave_scan((t + per - 1) / per), 63);
+    for (int b0 = 64; b0 < a->B; b0 += 64) n += read_lane(wave_scan((tiles_of_sequence(a, b0 + lane) + per - 1) / per), 63);
+    if (n * a->Hkv <= a->workers) break;
+    per += per / 8 + 1;
+  }
+  u0 = 0;
+  for (int b0 = 0; b0 < a->B; b0 += 64) {
+    if (b0 > 0) t = tiles_of_sequence(a, b0 + lane);
+    const int n = (t + per - 1) / per, upto = wave_scan(n * a->Hkv), all = read_lane(upto, 63);
+    if (u >= 0 ? u < u0 + all : p.b < b0 + 64) {
+      const int l = u >= 0 ? __builtin_ctzll(__ballot(upto > u - u0)) : p.b - b0;
+      p.b = b0 + l;
+      p.n = read_lane(n, l);
+      u0 += read_lane(upto, l) - p.n * a->Hkv;
+      if (u >= 0) { p.index = divide(u - u0, a->by_Hkv); p.kvh = u - u0 - p.index * a->Hkv; }
+      return true;
+    }
+    u0 += all;
+  }
+  return false;
+}
+
 template <int D, int RB, int NW, bool FLAT>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tile_kernel(PagedArgs) {
   constexpr int NST = NW == 8 ? 3 : 2, WROWS = 16 * RB;
@@ -155,7 +199,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
   // ---- this workgroup's tiles
   Unit nxt;
-  int left;                                        // tiles still to do
+  int left, row_base = 0;                          // tiles still to do; first query row
   long long slot = 2LL * blockIdx.x;               // of its partial results
   {
     const Args a = arguments();
@@ -168,18 +212,28 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         left = open_share<kTK>(blockIdx.x, nxt);
       }
     } else {
-      // The row tiles of a (sequence, K/V head, part), last rows first, run one after the other on one XCD, whose L2 brings them K and V
-      // once; heads that do not go round the XCDs evenly are cut into `cuts` lists of every so many-th row tile.
-      const int xcd = blockIdx.x % kNumXCDs, at = blockIdx.x / kNumXCDs, list = (a->row_tiles + a->cuts - 1) / a->cuts;
-      const int v = at / list * kNumXCDs + xcd, unit = v / a->cuts, rank = (at % list) * a->cuts + v % a->cuts;
-      if (unit >= a->B * a->Hkv * a->parts || rank >= a->row_tiles) return;
-      const int bh = unit / a->parts, part = unit - bh * a->parts;
-      const int b = divide(bh, a->by_Hkv);
-      open_unit<kTK>(nxt, b * a->row_tiles + a->row_tiles - 1 - rank, bh - b * a->Hkv, 0);
-      const int per = max((nxt.T + a->parts - 1) / a->parts, a->min_tiles);
-      nxt.i = part * per;
-      left = min(per, nxt.T - nxt.i);
-      slot = (long long)bh * a->parts + part;
+      // The row tiles of a (sequence, K/V head, part) run one after the other on one XCD, whose L2 brings them K and V once
+      const int xcd = blockIdx.x % kNumXCDs, at = blockIdx.x / kNumXCDs;
+      if (a->min_tiles == 0) {
+        // last rows first; heads that do not go round the XCDs evenly are cut into `cuts` lists of every so many-th row tile
+        const int list = (a->row_tiles + a->cuts - 1) / a->cuts;
+        const int v = at / list * kNumXCDs + xcd, bh = v / a->cuts, rank = (at % list) * a->cuts + v % a->cuts;
+        if (bh >= a->B * a->Hkv || rank >= a->row_tiles) return;
+        const int b = divide(bh, a->by_Hkv);
+        open_unit<kTK>(nxt, b * a->row_tiles + a->row_tiles - 1 - rank, bh - b * a->Hkv, 0);
+        left = nxt.T;
+      } else {
+        const int g8 = divide(at, a->by_row_tiles), rt = at - g8 * a->row_tiles, u = g8 * kNumXCDs + xcd;
+        Part p;
+        int u0;
+        if (!find_part(u, p, u0)) return;
+        open_unit<kTK>(nxt, p.b * a->row_tiles + rt, p.kvh, 0);
+        const int per = (nxt.T + p.n - 1) / p.n;
+        nxt.i = p.index * per;
+        left = min(per, nxt.T - nxt.i);
+        slot = u;
+      }
+      row_base = nxt.rt * a->tile_rows;
     }
   }
   if (left <= 0) return;
@@ -257,15 +311,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   int stage = 0;
   while (left > 0) {
     // ---- a unit
-    const int begin = cur.i;
-    int wave_row;                                  // the wave's first query row
+    const int begin = cur.i, wave_row = row_base + wave * WROWS;
     Rows<D, RB> w;
     int wg_hi, wg_lo;                              // ... of the workgroup's rows
     int all_lo, all_hi;                            // keys that all of the wave's rows see: [all_lo, all_hi) as far as they exist
     {
       const Args a = arguments();
       const int g = a->g, last_row = cur.s.q_len * g - 1;
-      wave_row = cur.rt * a->tile_rows + wave * WROWS;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int R = min(wave_row + 16 * rb + l16, last_row), r = divide(R, a->by_g), hq = cur.kvh * g + R - r * g;
@@ -334,7 +386,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const Args a = arguments();
     const bool whole = begin == 0 && i == cur.T;
     const int g = a->g, last_row = cur.s.q_len * g - 1;
-    const long long slot0 = FLAT ? (slot - cur.rt) * a->tile_rows : slot * a->R;   // of row 0
+    const long long slot0 = slot * a->R;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float l = w.lsum[rb];
@@ -371,28 +423,45 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
 // Merges the parts of a row that a row tile's workgroups left, in the order of the keys: D / 4 lanes per row
 template <int D>
-__global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int rows_wg) {
+__global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs) {
   const Args a = arguments();
   constexpr int TPR = D / 4, RPB = 256 / TPR;
-  const long long at = (long long)blockIdx.x * RPB + threadIdx.x / TPR;
-  if (at >= (long long)a->B * a->Hkv * a->R) return;
-  const int bh = (int)(at / a->R), R = (int)(at - (long long)bh * a->R), b = divide(bh, a->by_Hkv), kvh = bh - b * a->Hkv;
-  const int base = R / rows_wg * rows_wg;
-  const Seen s = seen_by(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, divide(base, a->by_g), divide(base + rows_wg - 1, a->by_g), kTK);
+  const int per_unit = (a->R + RPB - 1) / RPB, unit = blockIdx.x / (unsigned)per_unit;
+  Part p;
+  p.b = divide(unit, a->by_Hkv);
+  const int b = p.b, kvh = unit - b * a->Hkv;
+  int u0;
+  find_part(-1, p, u0);
+  const int R = (blockIdx.x - unit * per_unit) * RPB + threadIdx.x / TPR, rt = divide(R, a->by_tile_rows);
+  const Seen s = entry_seen<kTK>(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, rt);
   if (R >= s.q_len * a->g) return;
-  const int T = max(s.tiles, 1), per = max((T + a->parts - 1) / a->parts, a->min_tiles), n = (T + per - 1) / per;
+  const int T = tiles_to_do(a, s, rt), per = (T + p.n - 1) / p.n, n = (T + per - 1) / per;
   if (n == 1) return;                              // written by its workgroup
   const int d = (threadIdx.x % TPR) * 4;
   float M = kNegBig, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < n; ++k) {
-    const long long slot = ((long long)bh * a->parts + k) * a->R + R;
-    const f32x4 ov = *reinterpret_cast<const f32x4*>(a->ws_o + slot * D + d);
-    const float mk = a->ws_ml[2 * slot], lk = a->ws_ml[2 * slot + 1];
+  auto slot = [&](int k) { return (u0 + k * a->Hkv + kvh) * (long long)a->R + R; };
+  auto add = [&](float mk, float lk, const f32x4& ov) {
     const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
     acc = acc * c0 + ov * c1;
     l = l * c0 + lk * c1;
     M = up;
+  };
+  int k = 0;
+  for (; k + 4 <= n; k += 4) {                     // four parts' loads together
+    f32x4 ov[4]; float mk[4], lk[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const long long at = slot(k + x);
+      ov[x] = *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d);
+      mk[x] = a->ws_ml[2 * at]; lk[x] = a->ws_ml[2 * at + 1];
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) add(mk[x], lk[x], ov[x]);
+  }
+  for (; k < n; ++k) {
+    const long long at = slot(k);
+    add(a->ws_ml[2 * at], a->ws_ml[2 * at + 1], *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d));
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
@@ -406,12 +475,12 @@ __global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs, int r
 // Rows of a workgroup and the sharing of the work by rows R per (sequence, K/V head) (us; lengths 500 to 8000, 8 sequences, heads of
 // 128 unless stated):
 //   up to 64: four waves of 16 rows, equal shares: 32 heads of 64 rows 130, in parts 145; 28 and 4 heads, 16 rows a head (R = 112) 40, in
-//     parts 34
-//   up to 256: four waves of 32 rows, in parts, whose row tiles find K and V in L2: R = 224 40 us, eight waves in shares 47; 32
-//     sequences of 100 to 4000, R = 256, 126 and 168
+//     parts 33
+//   up to 256: four waves of 32 rows, in parts, whose row tiles find K and V in L2: R = 224 39 us, eight waves in shares 47; 32
+//     sequences of 100 to 4000, R = 256, 129 and 168
 //   more: eight waves of 32 rows, so that K and V come from L2 half as often: 2 x 2048 rows of 32 / 8 heads behind 4096 keys 321, four
 //     waves 344; 8 x 512 rows over 4096 keys 257 and 271 (heads of 64: 188 and 190)
-struct TilePlan { int rb, waves, flat, parts, tile_rows, row_tiles, cuts, min_tiles; SharePlan shares; };
+struct TilePlan { int rb, waves, flat, tile_rows, row_tiles, cuts; SharePlan shares; long long slots; };   // slots: parts at most
 
 static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   const long long R = (long long)p.Hq / p.Hkv * p.K, units = (long long)p.B * p.Hkv;
@@ -422,29 +491,29 @@ static TilePlan plan_tile(const sdllm_paged_attn_params& p, bool with_block) {
   pl.row_tiles = (int)((R + rows - 1) / rows);
   pl.tile_rows = rows;
   pl.flat = R <= 64;
-  pl.parts = pl.cuts = 1;
+  pl.cuts = 1;
   if (pl.flat) {
     pl.tile_rows = (int)R;
     pl.shares = plan_shares(p, with_block, pl.tile_rows, 1, kTK, at_once, 2);
     return pl;
   }
-  const long long tiles = paged_most_tiles(p, with_block, rows, kTK);
-  pl.min_tiles = p.kv_splits > 0 ? (int)((tiles + p.kv_splits - 1) / p.kv_splits) : 2;
-  long long parts = p.kv_splits > 0 ? p.kv_splits : at_once / (units * pl.row_tiles);
-  long long most = (tiles + pl.min_tiles - 1) / pl.min_tiles;
-  if (most * units * pl.row_tiles > (1 << 20)) most = (1 << 20) / (units * pl.row_tiles);   // workgroups, and what the merge has to read
-  if (parts > most) parts = most;
-  if (parts < 1) parts = 1;
-  pl.parts = (int)parts;
-  while (pl.cuts < kNumXCDs && (p.Hkv * parts * pl.cuts) % kNumXCDs != 0) pl.cuts *= 2;
+  const long long tiles = paged_most_tiles(p, with_block, rows, kTK), tiled = units * pl.row_tiles;
+  const long long most = (1 << 20) / tiled;        // workgroups, and what the merge has to read, stay bounded
+  const long long per = p.kv_splits > 0 ? (tiles + std::min<long long>(p.kv_splits, std::max(most, 1LL)) - 1) / std::min<long long>(p.kv_splits, std::max(most, 1LL)) : 2;
+  if (tiles > per && p.B <= 2048 && units * R < (1 << 23) && (p.kv_splits > 0 || tiled < at_once)) {
+    const long long workers = p.kv_splits > 0 ? 1 << 30 : at_once / pl.row_tiles;
+    pl.shares = SharePlan{(int)workers, (int)per};
+    pl.slots = std::min(units * ((tiles + per - 1) / per), workers);
+    return pl;
+  }
+  while (pl.cuts < kNumXCDs && pl.cuts < pl.row_tiles && p.Hkv * pl.cuts % kNumXCDs != 0) pl.cuts *= 2;
   return pl;
 }
 
 size_t paged_tile_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
   const TilePlan pl = plan_tile(p, with_block);
-  const size_t R = (size_t)(p.Hq / p.Hkv) * p.K;
   if (pl.flat) return share_bytes(pl.shares, pl.tile_rows, p.D);
-  return pl.parts == 1 ? 0 : (size_t)p.B * p.Hkv * pl.parts * R * (p.D + 2) * sizeof(float);
+  return (size_t)pl.slots * (p.Hq / p.Hkv * p.K) * (p.D + 2) * sizeof(float);
 }
 
 template <int D, int RB, int NW, bool FLAT>
@@ -475,28 +544,26 @@ hipError_t prepare_paged_tile() {
 
 hipError_t launch_paged_tile(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
   const TilePlan pl = plan_tile(p, a.kb != nullptr);
-  const int rows_wg = 16 * pl.rb * pl.waves;
   long long grid;
-  bool merge;
+  set_shares(a, pl.shares, pl.tile_rows, pl.row_tiles, p.D, workspace);
+  a.by_tile_rows = FastDiv(pl.tile_rows);
+  a.cuts = pl.cuts;
+  const long long units = (long long)p.B * p.Hkv;
   if (pl.flat) {
-    set_shares(a, pl.shares, pl.tile_rows, pl.row_tiles, p.D, workspace);
     grid = pl.shares.workers;
-    merge = pl.shares.min_tiles > 0;
+  } else if (pl.shares.min_tiles > 0) {
+    a.ws_ml = a.ws_o + (size_t)pl.slots * a.R * p.D;
+    grid = (pl.slots + kNumXCDs - 1) / kNumXCDs * kNumXCDs * pl.row_tiles;
   } else {
-    const size_t slots = (size_t)p.B * p.Hkv * pl.parts;
-    a.tile_rows = pl.tile_rows; a.row_tiles = pl.row_tiles; a.by_row_tiles = FastDiv(pl.row_tiles); a.parts = pl.parts; a.cuts = pl.cuts; a.min_tiles = pl.min_tiles;
-    merge = pl.parts > 1;
-    a.ws_o = merge ? (float*)workspace : nullptr;
-    a.ws_ml = merge ? a.ws_o + slots * a.R * p.D : nullptr;
-    grid = ((long long)slots * pl.cuts + kNumXCDs - 1) / kNumXCDs * kNumXCDs * ((pl.row_tiles + pl.cuts - 1) / pl.cuts);
+    grid = (units * pl.cuts + kNumXCDs - 1) / kNumXCDs * kNumXCDs * ((pl.row_tiles + pl.cuts - 1) / pl.cuts);
   }
   hipError_t e = p.D == 128 ? launch_tile_d<128>(a, pl, (unsigned)grid, stream) : launch_tile_d<64>(a, pl, (unsigned)grid, stream);
-  if (e != hipSuccess || !merge) return e;
+  if (e != hipSuccess || pl.shares.min_tiles == 0) return e;
   if (pl.flat) return launch_shares_merge(a, p.dtype, p.D, kTK, stream);
   const int rpb = 256 / (p.D / 4);
-  const unsigned blocks = (unsigned)(((long long)a.B * a.Hkv * a.R + rpb - 1) / rpb);
-  if (p.D == 128) hipLaunchKernelGGL(paged_parts_merge_kernel<128>, dim3(blocks), dim3(256), 0, stream, a, rows_wg);
-  else hipLaunchKernelGGL(paged_parts_merge_kernel<64>, dim3(blocks), dim3(256), 0, stream, a, rows_wg);
+  const unsigned blocks = (unsigned)(units * ((a.R + rpb - 1) / rpb));
+  if (p.D == 128) hipLaunchKernelGGL(paged_parts_merge_kernel<128>, dim3(blocks), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(paged_parts_merge_kernel<64>, dim3(blocks), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
