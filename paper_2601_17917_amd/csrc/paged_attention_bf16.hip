@@ -9,10 +9,13 @@
 //   S^T = K Q^T, O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, operands laid out as in the dense kernel (rows padded to 16 or 32).
 //   Online softmax: the product's accumulators start at minus the row's reference, so that it yields s - reference and a weight is
 //   one multiply and one exponential, whatever the scores' size; the reference moves only where a maximum exceeds it by 8 in log2
-//   units.
+//   units.  Weights are rounded to bf16 (2^-8 relative) for the second product, and the row sums are those of the rounded weights;
+//   all sums are fp32.
 // A (sequence, head) that one wave walked alone is written at once; of the others every wave leaves (O, m, l), merged in tile order
 // by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
 //   TOGETHER: the eight waves of a workgroup share the tiles of one (sequence, K/V head) and merge through LDS: no second launch.
+// Measured, one row over 32 and 8 heads of 128: 32 sequences of 200 to 16384 keys, 501 MB, 81 + 6 us (5.8 TB/s); 64 of 4096, 1.07 GB,
+// 170 us (6.3 TB/s); one of 700, 7.6 us; one of 32768, 134 MB, 35 us.
 #include "paged_attention.h"
 
 namespace sdllm {

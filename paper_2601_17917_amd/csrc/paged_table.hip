@@ -4,6 +4,7 @@
 // Extend is three prefix sums over the batch -- pages given back, pages needed, pages granted so far -- and a fill of the tables
 // and slots they decide.  It moves a few bytes per row, so what it costs is launches and dependent round trips: one workgroup
 // does the scans and, where there are few rows, the fill behind them; many rows are filled by a second launch over the chip.
+// Measured: 8 sequences of one row 2.0 us in the kernel; 64 of up to 2048 rows, a third of them new, 6.0 + 3.8 us.
 #include "paged_common.h"
 
 namespace sdllm {
