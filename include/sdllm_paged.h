@@ -75,7 +75,7 @@ int sdllm_paged_extend(const sdllm_paged_extend_params* p,
  *     original_len == 0:  f_i / s for every pair
  *     original_len  > 0:  u f_i + (1 - u) f_i / s, where r = f_i * original_len / (2 pi) is the number of turns of pair i in the
  *                         original context and u = clamp((r - low_turns) / (high_turns - low_turns), 0, 1)
- * Position of row t of sequence b: positions[b] + t, or positions[b * K + t] if positions_per_row.  The angle is formed in
+ * Position of row t of sequence b: positions[b] + t (which may pass 2^31), or positions[b * K + t] if positions_per_row.  The angle is formed in
  * double precision and reduced there, cos / sin, norm and products are fp32, the result is rounded once.
  *
  *   dtype, B, K >= 1 (B * K < 2^24), Hq, Hkv 1..65535, D (multiple of 16, <= 256), rotary_dim (multiple of 16, 0..D; 0: no rotation)
@@ -150,7 +150,7 @@ int sdllm_paged_kv_append(const sdllm_paged_append_params* p,
  *   page_size, n_pages, max_pages (entries of a table row, > 0); a page of all heads below 2 GiB
  *   max_kv_len      upper bound of kv_lens, <= max_pages * page_size: the launch plan is made for it (the lengths themselves are
  *                   device data); max_kv_len + K <= 2^30
- *   scale           softmax scale; <= 0 selects 1/sqrt(D)
+ *   scale           softmax scale, at most 1e38; <= 0 selects 1/sqrt(D)
  *   kv_splits       0 = choose automatically; n >= 1: a sequence of max_kv_len keys is cut into about n parts, if the batch is not so
  *                   large that parts gain nothing
  *   *_stride        as for sdllm_qk_norm_rope
@@ -175,7 +175,7 @@ size_t sdllm_paged_attention_workspace_bytes(const sdllm_paged_attn_params* p, i
  *   q [B,Hq,K,D] read    k_pages, v_pages [n_pages,Hkv,page_size,D] read    block_table [B,max_pages] int32, kv_lens [B] int32
  *   k_block, v_block [B,Hkv,K,D] read, both or neither      q_lens [B] int32 or NULL (= K)
  *   out [B,Hq,K,D]: rows r < q_lens[b] are written, the others left as they were
- * Inputs are only read.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ * Inputs are only read; out and workspace overlap none of them.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
  */
 int sdllm_paged_attention(const sdllm_paged_attn_params* p,
                           const void* q, const void* k_pages, const void* v_pages,

@@ -123,6 +123,7 @@ int check_paged_attn(const sdllm_paged_attn_params* p, bool with_block) {
   if (p->window < 0 || p->sinks < 0) return set_error(kInvalid, "%s: window and sinks must be >= 0", w);
   if (p->kv_splits < 0) return set_error(kInvalid, "%s: kv_splits must be >= 0", w);
   if (!(p->scale == p->scale) || std::isinf(p->scale)) return set_error(kInvalid, "%s: scale is not finite", w);
+  if (p->scale > 1e38f) return set_error(kUnsupported, "%s: scale is too large", w);       // its product with log2 e is an fp32 number
   const long long rows = (long long)p->Hq * p->K;
   if ((long long)p->max_kv_len + p->K > (1LL << 30) || (long long)p->B * p->Hkv >= (1LL << 22) || rows >= (1LL << 28) ||
       rows * p->B >= (1LL << 28) || (long long)p->B * p->max_pages > 0x7fffffffLL)

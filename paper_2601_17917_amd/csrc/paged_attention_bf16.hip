@@ -321,29 +321,35 @@ size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_
 }
 
 template <int D, int RB>
-static void launch_stream(const PagedArgs& a, bool one_unit, hipStream_t stream) {
-  constexpr int wave_bytes = StreamShape<D>::WAVEB;
-  if (one_unit) hipLaunchKernelGGL((paged_stream_kernel<D, RB, true>), dim3(a.workers), dim3(512), 8 * (wave_bytes + 128 * RB), stream, a);
-  else hipLaunchKernelGGL((paged_stream_kernel<D, RB, false>), dim3((a.workers + 3) / 4), dim3(256), 4 * wave_bytes, stream, a);
+static hipError_t launch_stream(const PagedArgs& a, bool one_unit, hipStream_t stream, bool launch = true) {
+  constexpr int wave_bytes = StreamShape<D>::WAVEB, together_bytes = 8 * (wave_bytes + 128 * RB);
+  static LdsOptIn st;
+  if (one_unit) {
+    hipError_t e = ensure_lds_opt_in(reinterpret_cast<const void*>(&paged_stream_kernel<D, RB, true>), together_bytes, st);
+    if (e != hipSuccess || !launch) return e;
+    hipLaunchKernelGGL((paged_stream_kernel<D, RB, true>), dim3(a.workers), dim3(512), together_bytes, stream, a);
+  } else {
+    hipLaunchKernelGGL((paged_stream_kernel<D, RB, false>), dim3((a.workers + 3) / 4), dim3(256), 4 * wave_bytes, stream, a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_stream(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
   const bool one_unit = together(p, a.kb != nullptr);
   set_shares(a, plan_stream(p, a.kb != nullptr), a.R, 1, p.D, workspace);
-  if (p.D == 128) a.R <= 16 ? launch_stream<128, 1>(a, one_unit, stream) : launch_stream<128, 2>(a, one_unit, stream);
-  else a.R <= 16 ? launch_stream<64, 1>(a, one_unit, stream) : launch_stream<64, 2>(a, one_unit, stream);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (p.D == 128) e = a.R <= 16 ? launch_stream<128, 1>(a, one_unit, stream) : launch_stream<128, 2>(a, one_unit, stream);
+  else e = a.R <= 16 ? launch_stream<64, 1>(a, one_unit, stream) : launch_stream<64, 2>(a, one_unit, stream);
   if (e != hipSuccess || a.min_tiles == 0) return e;
   return launch_shares_merge(a, p.dtype, p.D, 4096 / p.D, stream);
 }
 
-// Workgroups of more than 64 KiB of LDS have to be allowed once per device, outside any graph capture
 hipError_t prepare_paged_stream() {
-  const void* kernels[] = {(const void*)paged_stream_kernel<128, 1, true>, (const void*)paged_stream_kernel<128, 2, true>,
-                           (const void*)paged_stream_kernel<64, 1, true>, (const void*)paged_stream_kernel<64, 2, true>};
-  for (const void* k : kernels)
-    if (hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (16384 + 256)); e != hipSuccess) return e;
-  return hipSuccess;
+  hipError_t e = launch_stream<128, 1>(PagedArgs{}, true, nullptr, false);
+  if (e == hipSuccess) e = launch_stream<128, 2>(PagedArgs{}, true, nullptr, false);
+  if (e == hipSuccess) e = launch_stream<64, 1>(PagedArgs{}, true, nullptr, false);
+  if (e == hipSuccess) e = launch_stream<64, 2>(PagedArgs{}, true, nullptr, false);
+  return e;
 }
 
 }  // namespace sdllm

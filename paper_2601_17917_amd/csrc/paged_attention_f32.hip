@@ -262,24 +262,31 @@ size_t paged_f32_workspace_bytes(const sdllm_paged_attn_params& p, bool with_blo
 }
 
 template <int D>
-static void launch_f32(const PagedArgs& a, bool one_unit, hipStream_t stream) {
-  if (one_unit) hipLaunchKernelGGL((paged_f32_kernel<D, true>), dim3(a.workers), dim3(512), 8 * 16 * (D + 2) * sizeof(float), stream, a);
-  else hipLaunchKernelGGL((paged_f32_kernel<D, false>), dim3((a.workers + 3) / 4), dim3(256), 0, stream, a);
+static hipError_t launch_f32(const PagedArgs& a, bool one_unit, hipStream_t stream, bool launch = true) {
+  constexpr size_t together_bytes = 8 * 16 * (D + 2) * sizeof(float);
+  static LdsOptIn st;
+  if (one_unit) {
+    hipError_t e = ensure_lds_opt_in(reinterpret_cast<const void*>(&paged_f32_kernel<D, true>), together_bytes, st);
+    if (e != hipSuccess || !launch) return e;
+    hipLaunchKernelGGL((paged_f32_kernel<D, true>), dim3(a.workers), dim3(512), together_bytes, stream, a);
+  } else {
+    hipLaunchKernelGGL((paged_f32_kernel<D, false>), dim3((a.workers + 3) / 4), dim3(256), 0, stream, a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_f32(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream) {
   const int row_tiles = row_tiles_of(p);
   const bool one_unit = together(p, a.kb != nullptr, row_tiles);
   set_shares(a, plan_f32(p, a.kb != nullptr), 16, row_tiles, p.D, workspace);
-  if (p.D == 128) launch_f32<128>(a, one_unit, stream);
-  else launch_f32<64>(a, one_unit, stream);
-  hipError_t e = hipGetLastError();
+  hipError_t e = p.D == 128 ? launch_f32<128>(a, one_unit, stream) : launch_f32<64>(a, one_unit, stream);
   if (e != hipSuccess || a.min_tiles == 0) return e;
   return launch_shares_merge(a, p.dtype, p.D, 16, stream);
 }
 
 hipError_t prepare_paged_f32() {
-  return hipFuncSetAttribute((const void*)paged_f32_kernel<128, true>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * 16 * 130 * sizeof(float));
+  hipError_t e = launch_f32<128>(PagedArgs{}, true, nullptr, false);
+  return e == hipSuccess ? launch_f32<64>(PagedArgs{}, true, nullptr, false) : e;
 }
 
 }  // namespace sdllm

@@ -83,8 +83,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
   };
   load(row0 + tid / GL);
   for (int i = tid; i < a.R / 2; i += 256) {
-    const int pos = a.per_row ? a.positions[token] : a.positions[b] + t;
-    const double x = (double)pos * a.turns[i];
+    const double pos = a.per_row ? (double)a.positions[token] : (double)a.positions[b] + t;    // a sum may pass 2^31
+    const double x = pos * a.turns[i];
     const float r = (float)(x - rint(x));
     float s, c;
     sincospif(2.0f * r, &s, &c);

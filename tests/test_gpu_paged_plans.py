@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from gpu_util import to_f64_host
-from oracle.paged import paged_extend as oracle_extend
+from oracle.paged import norm_rope as oracle_norm_rope, paged_extend as oracle_extend
 from paged_util import attention_problem, call_attention, check_attention, error_ratio, make_tables, oracle_outputs, SENTINEL
 
 pytestmark = pytest.mark.gpu
@@ -184,3 +184,23 @@ def test_norm_rope_of_many_rows(gpu_lib, dtype, interleaved):
         at = slice(t, min(t + 500, K))
         assert torch.equal(run(at, *pools[2:]), whole[:, :, at])
     assert torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3])
+
+
+def test_positions_that_pass_31_bits(gpu_lib):
+    """The first row's position fits the type, later ones need not.  Angles of 2^31 rad in double are off by 2^-53 2^31 = 2.4e-7 in the
+    oracle and in the kernel, 5e-7 together; the rest of a row's error is at most 2.1e-6 of the pair's sum (|q| <= 6: 12)."""
+    B, K, H, D = 2, 9, 3, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(33)
+    q = torch.randn((B, H, K, D), generator=g, device="cuda").clamp(-6, 6)
+    start = np.array([2 ** 31 - 4, -5], dtype=np.int32)
+    got, _ = gpu_lib.qk_norm_rope(q, q.clone(), dev(start), 1e4, eps=0.0, interleaved=True)
+    want = oracle_norm_rope(to_f64_host(q), None, start[:, None].astype(np.int64) + np.arange(K)[None], 1e4, interleaved=True)
+    assert np.abs(to_f64_host(got) - want).max() <= (2.1e-6 + 5e-7) * 12
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_largest_scale(gpu_lib, dtype):
+    """Weights of one and zero: the value of the key with the largest score."""
+    s = attention_problem(34, dtype, 2, 4, 2, 64, 2, 16, [90, 40], None, False)
+    check_attention(gpu_lib, s, dtype, scale=0.99e38)

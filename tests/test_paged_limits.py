@@ -36,3 +36,10 @@ def test_workspaces_at_the_limits(dtype, change, splits):
     assert n != INVALID and n <= (1 << 28) * (64 + 2) * 4
     if splits == 1:
         assert n == 0
+
+
+@pytest.mark.parametrize("scale", [1.01e38, 3.4e38])
+def test_scales_whose_product_with_log2_e_is_no_number(scale):
+    assert need(scale=scale) == INVALID
+    assert b"scale" in sd.load_library().sdllm_last_error()
+    assert need(scale=0.99e38) != INVALID
