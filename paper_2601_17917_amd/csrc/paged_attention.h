@@ -221,6 +221,11 @@ struct Pages {
     id = row[min(64 * want + fresh_lane(), h.last_page)];   // entries behind the table's end repeat the last one
     valid = __ballot((unsigned)id < (unsigned)h.n_pages);
   }
+  // keys [begin, valid_until) are in valid pages of these entries, one after the other
+  __device__ __forceinline__ int begin(const Hot& h) const { return block << (h.shift + 6); }
+  __device__ __forceinline__ int valid_until(const Hot& h) const {
+    return begin(h) + ((~valid == 0 ? 64 : __builtin_ctzll(~valid)) << h.shift);
+  }
   __device__ __forceinline__ int of(const Hot& h, int k) const { return __builtin_amdgcn_readlane(id, (k >> h.shift) & 63); }
   __device__ __forceinline__ bool ok(const Hot& h, int k) const { return (valid >> ((k >> h.shift) & 63)) & 1; }
   // all pages of the TK keys from k on (a multiple of TK)
@@ -249,13 +254,18 @@ template <int D> struct Slab {
     return r * ROWB + ((c ^ (v ? 2 * ((r / R256) % (CPR / 2)) : (r / R256) % CPR)) << 4);
   }
   __device__ static constexpr unsigned flips(bool v, int j) { return v ? (D == 128 ? 128 * (j & 1) : 0) : 64 * j; }
+  __device__ static __forceinline__ void offsets(bool v, unsigned (&off)[4]) {
+    const unsigned g = lane_offset(v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) off[j] = g ^ flips(v, j);
+  }
 };
 
 // Whole slab from consecutive rows; V: which tensor's order.  (The offsets are made here: kept over a loop they cost registers.)
 template <int D, bool ONCE, bool V>
 __device__ __forceinline__ void move_slab(unsigned lds, const unsigned char* src) {
-  const unsigned g = Slab<D>::lane_offset(V);
-  const unsigned off[4] = {g, g ^ Slab<D>::flips(V, 1), g ^ Slab<D>::flips(V, 2), g ^ Slab<D>::flips(V, 3)};
+  unsigned off[4];
+  Slab<D>::offsets(V, off);
   dma_slab<Slab<D>::IPT, ONCE>(lds, uniform_ptr(src), off);
 }
 

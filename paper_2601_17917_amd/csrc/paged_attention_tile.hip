@@ -58,14 +58,14 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
   // their side of these barriers, other arithmetic need not)
   bf16x8 kop[4][NS];
 #pragma unroll
-  for (int kb = 0; kb < 4; ++kb)
+  for (int s2 = 0; s2 < NS; ++s2)
 #pragma unroll
-    for (int s2 = 0; s2 < NS; ++s2) kop[kb][s2] = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
+    for (int kb = 0; kb < 4; ++kb) kop[kb][s2] = *(lds_bf16x8_ptr)(uintptr_t)((kro ^ (s2 << 6)) + kb * S::SLABB);
   __builtin_amdgcn_sched_barrier(0x406);
 #pragma unroll
-  for (int kb = 0; kb < 4; ++kb)
+  for (int s2 = 0; s2 < NS; ++s2)
 #pragma unroll
-    for (int s2 = 0; s2 < NS; ++s2)
+    for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) sacc[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[kb][s2], w.q[rb][s2], sacc[rb][kb], 0, 0, 0);
   // the values of the tile's first half travel under the softmax
@@ -253,14 +253,32 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const unsigned vro = lds0 + S::VB + (4 * G + e4) * ROWB + (((c4 >> 1) ^ fv) << 4) + ((c4 & 1) << 3);
   const unsigned lds_slab = lds0 + slab * S::SLABB;
 
+  // Tiles of nxt's unit that start at keys [plain, plain + plain_span] are whole, cached, and in valid pages of the 64 entries at hand:
+  // one comparison and an address for most tiles.  (Eight waves that each go through all the conditions below cost a tile 400 cycles.)
+  int plain = 0x7fffffff;
+  unsigned plain_span = 0;
+  unsigned k_off[4], v_off[4];                     // the lane's offsets within a slab
+  Slab<D>::offsets(false, k_off);
+  Slab<D>::offsets(true, v_off);
   // Puts the tile at nxt in flight into ring stage `stage`; returns which of its keys some query row sees.  A tile that is not whole
-  // has landed on return (its transfers are not counted: step_wait).
+  // has landed on return (its transfers are not counted).
   auto issue = [&](int stage) -> unsigned long long {
     const Seen& s = nxt.s;
     const int k0 = s.tile(nxt.i) * kTK, k = k0 + 16 * slab;
-    pages.seek(h, k0);
-    const unsigned long long at = row_offset(h, pages.of(h, k), nxt.kvh, k, ROWB);
     const unsigned to = lds_slab + stage * S::STAGEB;
+    if ((unsigned)(k0 - plain) <= plain_span) {
+      const unsigned long long at = row_offset(h, pages.of(h, k), nxt.kvh, k, ROWB);
+      if (NW == 4 || kind == 0) dma_slab<Slab<D>::IPT, ONCE>(to, uniform_ptr(h.kp + at), k_off);
+      if (NW == 4 || kind == 1) dma_slab<Slab<D>::IPT, ONCE>(to + S::VB, uniform_ptr(h.vp + at), v_off);
+      return ~0ull;
+    }
+    pages.seek(h, k0);
+    {
+      const int lo = max(s.lo, pages.begin(h)), hi = min(s.last16 + 16, pages.valid_until(h)) - kTK;
+      plain = hi >= lo && s.tiles > 0 ? lo : 0x7fffffff;
+      plain_span = hi >= lo ? hi - lo : 0;
+    }
+    const unsigned long long at = row_offset(h, pages.of(h, k), nxt.kvh, k, ROWB);
     if (s.tiles > 0 && pages.all_ok<kTK>(h, k0) && ((k0 >= s.lo && k0 + kTK - 16 <= s.last16) || k0 + kTK - 16 <= s.sink16)) {
       if constexpr (NW == 8) {
         if (kind == 0) move_slab<D, ONCE, false>(to, h.kp + at);
@@ -290,7 +308,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const int b = nxt.b, kvh = nxt.kvh;
       next_tile<kTK>(nxt);
       if (nxt.b != b) pages.open(nxt.b);
-      if (nxt.b != b || nxt.kvh != kvh) block.open(nxt.b, nxt.kvh);
+      if (nxt.b != b || nxt.kvh != kvh) {
+        block.open(nxt.b, nxt.kvh);
+        plain = 0x7fffffff; plain_span = 0;
+      }
     } else {
       ++nxt.i;
     }
