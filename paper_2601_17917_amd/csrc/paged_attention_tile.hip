@@ -272,6 +272,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       if (NW == 4 || kind == 1) dma_slab<Slab<D>::IPT, ONCE>(to + S::VB, uniform_ptr(h.vp + at), v_off);
       return ~0ull;
     }
+    if (k0 >= s.n && k0 >= s.lo && k0 + kTK <= s.hi && block.k_stride != 0) {
+      const unsigned long long x = (unsigned)(k - s.n);
+      const unsigned char *kr = block.k + x * block.k_stride, *vr = block.v + x * block.v_stride;
+      if (block.k_stride == ROWB && block.v_stride == ROWB) {
+        if (NW == 4 || kind == 0) dma_slab<Slab<D>::IPT, ONCE>(to, uniform_ptr(kr), k_off);
+        if (NW == 4 || kind == 1) dma_slab<Slab<D>::IPT, ONCE>(to + S::VB, uniform_ptr(vr), v_off);
+      } else {
+        if (NW == 4 || kind == 0) move_strided<D, ONCE, false>(to, kr, block.k_stride);
+        if (NW == 4 || kind == 1) move_strided<D, ONCE, true>(to + S::VB, vr, block.v_stride);
+      }
+      return ~0ull;
+    }
     pages.seek(h, k0);
     {
       const int lo = max(s.lo, pages.begin(h)), hi = min(s.last16 + 16, pages.valid_until(h)) - kTK;
@@ -287,12 +299,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         move_slab<D, ONCE, false>(to, h.kp + at);
         move_slab<D, ONCE, true>(to + S::VB, h.vp + at);
       }
-      return ~0ull;
-    }
-    if (k0 >= s.n && k0 >= s.lo && k0 + kTK <= s.hi && block.k_stride != 0) {
-      const unsigned long long x = (unsigned)(k - s.n);
-      if (NW == 4 || kind == 0) move_strided<D, ONCE, false>(to, block.k + x * block.k_stride, block.k_stride);
-      if (NW == 4 || kind == 1) move_strided<D, ONCE, true>(to + S::VB, block.v + x * block.v_stride, block.v_stride);
       return ~0ull;
     }
     const unsigned long long vis = seen_keys<kTK>(h, s, pages, k0);    // rows that see nothing: none
