@@ -5,7 +5,7 @@
 // -- sequences, their K/V heads, their tiles, laid end to end -- so that all waves carry the same number of tiles whatever the
 // lengths are, and meets no other wave.  A tile (8 KiB of K and 8 KiB of V) goes global -> LDS into the wave's own 16 KiB, from
 // there into registers in operand layout, and the next tile's transfers go in flight into the same 16 KiB while the products and
-// the softmax of this one run: with eight waves on a CU some 100 KiB are in flight all the time.
+// the softmax of this one run.
 //   S^T = K Q^T, O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, operands laid out as in the dense kernel (rows padded to 16 or 32).
 //   Online softmax: the product's accumulators start at minus the row's reference, so that it yields s - reference and a weight is
 //   one multiply and one exponential, whatever the scores' size; the reference moves only where a maximum exceeds it by 8 in log2
@@ -299,7 +299,10 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
   }
 }
 
-static constexpr int kStreamWaves = 8 * kNumCUs;   // resident at once: two workgroups of 64 KiB per CU
+// Waves that share the tiles: one to a SIMD.  Two fit, but do not read faster, and leave twice as much to merge (us, one and two: 1 sequence
+// of 16384 keys, 32 / 8 heads of 128, 21 / 23; 32 sequences of 8192 168 / 168; 28 / 4 heads, 4 rows, 32 sequences of 8000 96 / 105).
+// A share has two tiles at least: of one, 1 sequence of 2048 keys 11.6 against 12.1, of 4096 13.8 against 13.2; of three 14.1, 14.8.
+static constexpr int kStreamWaves = 4 * kNumCUs;
 static constexpr int kStreamMinTiles = 2;
 // Waves of a workgroup together, or each for itself (us, 32 query and 8 K/V heads of 128, one row each; together / for itself):
 //   up to 4 units per CU: few keys, where a second launch for the merge costs more than idle CUs do, or no fewer workgroups busy:

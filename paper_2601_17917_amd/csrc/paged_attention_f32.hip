@@ -254,7 +254,9 @@ static int row_tiles_of(const sdllm_paged_attn_params& p) { return (int)(((long 
 static SharePlan plan_f32(const sdllm_paged_attn_params& p, bool with_block) {
   const int row_tiles = row_tiles_of(p);
   if (together(p, with_block, row_tiles)) return SharePlan{p.B * p.Hkv * row_tiles, 0};
-  return plan_shares(p, with_block, 16, row_tiles, 16, 8 * kNumCUs, 4);
+  // Heads of 64 (half the work and the bytes of a tile): two waves to a SIMD and four tiles a share, else one and two.  (us, one and two to
+  // a SIMD: 4 sequences of 20000 keys, 16 / 4 heads of 64, 5 rows 68 / 60; 16 of 4096, 32 / 8 heads of 128, 1 row 102 / 107, 1 of 1000 14 / 18.)
+  return p.D == 64 ? plan_shares(p, with_block, 16, row_tiles, 16, 8 * kNumCUs, 4) : plan_shares(p, with_block, 16, row_tiles, 16, 4 * kNumCUs, 2);
 }
 
 size_t paged_f32_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block) {
