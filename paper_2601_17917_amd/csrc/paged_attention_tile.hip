@@ -9,8 +9,8 @@
 //   else: a workgroup per (row tile, sequence, K/V head), the tiles of the last rows, which see most under a causal mask, first; or,
 //         where that is fewer than fit on the chip, per (row tile, sequence, K/V head, part of the keys).  Sequences get parts by their
 //         lengths: parts have as few tiles as let all workgroups be on the chip at once.
-// Many rows are bound by the matrix cores and the softmax between them: 8 x 512 rows of 32 / 8 heads over 4096 keys 257 us (1.07
-// PFLOP/s), 2 x 2048 causal rows behind 4096 keys 321 us (1.07).  Blocks, 28 and 4 heads of 32 rows, 8 sequences of 500 to 8000 keys: 28 us
+// Many rows are bound by the matrix cores and the softmax between them: 8 x 512 rows of 32 / 8 heads over 4096 keys 255 us (1.08
+// PFLOP/s), 2 x 2048 causal rows behind 4096 keys 310 us (1.11).  Blocks, 28 and 4 heads of 32 rows, 8 sequences of 500 to 8000 keys: 28 us
 // and 8 us in the merge, of which a workgroup's start (its place, table, queries, the first two tiles) and end are 10.
 #include "paged_attention.h"
 #include <algorithm>
