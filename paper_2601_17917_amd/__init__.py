@@ -71,6 +71,7 @@ class RopeParams(ctypes.Structure):
 
 
 _Stride = ctypes.c_int64 * 3
+_DENSE = _Stride(0, 0, 0)
 
 
 class PagedExtendParams(ctypes.Structure):
@@ -614,7 +615,7 @@ def _strides(t, name, shape, dtype):
     if t.shape != shape:
         raise SdllmError(ERR_INVALID_ARG, f"{name} must be {list(shape)}, is {list(t.shape)}")
     if t.is_contiguous():
-        return _Stride(0, 0, 0)
+        return _DENSE
     b, h, k, last = t.stride()
     nb, nh, nk, _ = shape
     if last != 1:
@@ -702,13 +703,12 @@ def bind_qk_norm_rope(q, k, positions, theta_base: float, q_weight=None, k_weigh
     _shaped(positions, "positions", (B, K) if per_row else (B,), torch.int32)
     _shaped(q_weight, "q_weight", (D,), dtype)
     _shaped(k_weight, "k_weight", (D,), dtype)
-    dense = _Stride(0, 0, 0)
     heads, keys = (B, Hq, K, D), (B, Hkv, K, D)
     p = QkNormRopeParams(_dtype_code(q), B, K, Hq, Hkv, D, D if rotary_dim is None else rotary_dim, int(bool(interleaved)),
                          int(per_row), page_size, n_pages, eps, theta_base, scale_factor, low_turns, high_turns, amplitude,
                          original_len, _strides(q, "q", heads, dtype), _strides(k, "k", keys, dtype),
-                         dense if v is None else _strides(v, "v", keys, dtype), _strides(q_out, "q_out", heads, dtype),
-                         dense if k_out is None else _strides(k_out, "k_out", keys, dtype))
+                         _DENSE if v is None else _strides(v, "v", keys, dtype), _strides(q_out, "q_out", heads, dtype),
+                         _DENSE if k_out is None else _strides(k_out, "k_out", keys, dtype))
     tensors = (q, k, v, positions, q_weight, k_weight, q_out, k_out, k_pages, v_pages, slots)
     _on_current_device(*tensors)
     args = (ctypes.byref(p), *map(_ptr, tensors), _stream(stream))
@@ -780,12 +780,11 @@ def bind_paged_attention(q, k_pages, v_pages, block_table, kv_lens, max_kv_len: 
     _shaped(q_lens, "q_lens", (B,), torch.int32)
     block = k_block is not None
     heads, keys = (B, Hq, K, D), (B, Hkv, K, D)
-    dense = _Stride(0, 0, 0)
     p = paged_attn_params(_dtype_code(q), B, Hq, Hkv, D, K, page_size, n_pages, block_table.shape[1], max_kv_len, causal, window,
                           sinks, scale, kv_splits, q_stride=_strides(q, "q", heads, dtype),
                           out_stride=_strides(out, "out", heads, dtype),
-                          k_block_stride=_strides(k_block, "k_block", keys, dtype) if block else dense,
-                          v_block_stride=_strides(v_block, "v_block", keys, dtype) if block else dense)
+                          k_block_stride=_strides(k_block, "k_block", keys, dtype) if block else _DENSE,
+                          v_block_stride=_strides(v_block, "v_block", keys, dtype) if block else _DENSE)
     need = paged_attention_workspace_bytes(p, block)
     if need and workspace is None:
         workspace = _new((need,), torch.uint8, q.device, stream)

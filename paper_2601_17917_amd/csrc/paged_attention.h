@@ -235,6 +235,17 @@ struct Pages {
     return ((valid >> ((k >> h.shift) & 63)) & want) == want;
   }
 };
+// Opens a unit whose number is known from the start: its lengths and its first table entries travel together
+template <int TK>
+__device__ __forceinline__ void open_whole_unit(Unit& u, Pages& pages, const Hot& h, int unit) {
+  const Args a = arguments();
+  const const_i32_ptr lens = (const_i32_ptr)(uintptr_t)a->lens, q_lens = (const_i32_ptr)(uintptr_t)a->q_lens;
+  const int e = divide(unit, a->by_Hkv), b = divide(e, a->by_row_tiles);
+  const int n = lens[b], q_len = a->q_lens ? q_lens[b] : a->K;
+  pages.open(b);
+  pages.seek(h, 0);
+  open_unit<TK>(u, e, unit - e * a->Hkv, 0, n, q_len);
+}
 // Byte offset in kp / vp of row k of K/V head kvh, which lies in page id
 __device__ __forceinline__ unsigned long long row_offset(const Hot& h, int id, int kvh, int k, int row_bytes) {
   return (unsigned long long)(unsigned)id * h.page_bytes + (unsigned)(((kvh << h.shift) + (k & ((1 << h.shift) - 1))) * row_bytes);

@@ -67,17 +67,19 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
 
   // this wave's tiles
   const int worker = TOGETHER ? blockIdx.x : blockIdx.x * NW + wave;
+  const Hot h = hot_arguments();
+  Pages pages;
   Unit nxt;
   int left;                                        // tiles of its share still to do
   {
     const Args a = arguments();
     if (worker >= a->workers) return;
     if (a->min_tiles == 0) {                       // a wave, or a workgroup, per (sequence, K/V head)
-      const int e = divide(worker, a->by_Hkv);
-      open_unit<TK>(nxt, e, worker - e * a->Hkv, 0);
+      open_whole_unit<TK>(nxt, pages, h, worker);
       left = nxt.T;
     } else {
       left = open_share<TK>(worker, nxt);
+      pages.open(nxt.b);
     }
   }
   [[maybe_unused]] int waves = 0;                  // of the workgroup that have tiles
@@ -96,9 +98,6 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
     }
   }
   if (left == 0) return;
-  const Hot h = hot_arguments();
-  Pages pages;
-  pages.open(nxt.b);
   const unsigned base = uniform((int)(unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)lds_wave);
   unsigned long long vis_next = issue_tile<D>(h, nxt, pages, base, lds_wave);
   // LDS offsets of the lane's operands of slice 0 / d block 0; the others flip bits of them

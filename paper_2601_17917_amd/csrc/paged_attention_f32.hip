@@ -25,17 +25,19 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_f32_kernel(Page
   const int lane = threadIdx.x & 63, l16 = lane & 15, G = lane >> 4;
   extern __shared__ __attribute__((aligned(16))) float part_s[];       // TOGETHER: (rows of D, then reference and sum) of each wave
   const int wave = uniform(threadIdx.x >> 6), worker = TOGETHER ? blockIdx.x : blockIdx.x * NW + wave;
+  const Hot h = hot_arguments();
+  Pages pages;
   Unit cur;
   int left;
   {
     const Args a = arguments();
     if (worker >= a->workers) return;
     if (a->min_tiles == 0) {
-      const int e = divide(worker, a->by_Hkv);
-      open_unit<TK>(cur, e, worker - e * a->Hkv, 0);
+      open_whole_unit<TK>(cur, pages, h, worker);
       left = cur.T;
     } else {
       left = open_share<TK>(worker, cur);
+      pages.open(cur.b);
     }
   }
   [[maybe_unused]] int waves = 0;                  // of the workgroup that have tiles
@@ -54,9 +56,6 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_f32_kernel(Page
     }
   }
   if (left == 0) return;
-  const Hot h = hot_arguments();
-  Pages pages;
-  pages.open(cur.b);
   int part = 0;
   while (left > 0) {
     const int begin = cur.i;
