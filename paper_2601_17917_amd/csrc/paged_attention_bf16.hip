@@ -15,7 +15,7 @@
 // by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
 //   TOGETHER: the eight waves of a workgroup share the tiles of one (sequence, K/V head) and merge through LDS: no second launch.
 // Measured, one row over 32 and 8 heads of 128: 32 sequences of 200 to 16384 keys, 501 MB, 80 + 5 us (5.8 TB/s); 64 of 4096, 1.07 GB,
-// 170 us (6.3 TB/s); one of 700, 7.6 us; one of 32768, 134 MB, 31 us.
+// 170 us (6.3 TB/s); one of 700, 7.1 us; one of 32768, 134 MB, 31 us.
 #include "paged_attention.h"
 
 namespace sdllm {

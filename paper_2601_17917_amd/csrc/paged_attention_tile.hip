@@ -10,7 +10,7 @@
 //         where that is fewer than fit on the chip, per (row tile, sequence, K/V head, part of the keys).  Sequences get parts by their
 //         lengths: parts have as few tiles as let all workgroups be on the chip at once.
 // Many rows are bound by the matrix cores and the softmax between them: 8 x 512 rows of 32 / 8 heads over 4096 keys 255 us (1.08
-// PFLOP/s), 2 x 2048 causal rows behind 4096 keys 310 us (1.11).  Blocks, 28 and 4 heads of 32 rows, 8 sequences of 500 to 8000 keys: 28 us
+// PFLOP/s), 2 x 2048 causal rows behind 4096 keys 307 us (1.12).  Blocks, 28 and 4 heads of 32 rows, 8 sequences of 500 to 8000 keys: 28 us
 // and 8 us in the merge, of which a workgroup's start (its place, table, queries, the first two tiles) and end are 10.
 #include "paged_attention.h"
 #include <algorithm>
@@ -149,37 +149,40 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
 
 // ---- Parts: u counts (sequence, part, K/V head) over the call.
 // Tiles that decide on the number of parts of sequence b: of its first or its last row tile, whichever has more
-__device__ __forceinline__ int tiles_of_sequence(Args a, int b) {
+__device__ __forceinline__ int tiles_of_sequence(Args a, int b, int& n, int& q_len) {
+  n = q_len = 0;
   if (b >= a->B) return 0;
-  const int n = a->lens[b], q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
+  n = a->lens[b];
+  q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
   if (q_len == 0) return 0;
   const int last = divide(q_len * a->g - 1, a->by_tile_rows);
   return max(tiles_to_do(a, entry_seen<kTK>(a, n, q_len, 0), 0), tiles_to_do(a, entry_seen<kTK>(a, n, q_len, last), last));
 }
-struct Part { int b, kvh, index, n; };             // part `index` of n
+struct Part { int b, kvh, index, n, len, q_len; }; // part `index` of n of a sequence
 // Number u0 of the first of a sequence's parts, for u >= 0 of the sequence that u belongs to, else of sequence p.b; false: none
 __device__ __forceinline__ bool find_part(int u, Part& p, int& u0) {
   const Args a = arguments();
   const int lane = threadIdx.x & 63;
-  int t = tiles_of_sequence(a, lane);
+  int len, q_len, unused[2];
+  int t = tiles_of_sequence(a, lane, len, q_len);
   long long total = read_lane(wave_scan(t), 63);
-  for (int b0 = 64; b0 < a->B; b0 += 64) total += read_lane(wave_scan(tiles_of_sequence(a, b0 + lane)), 63);
+  for (int b0 = 64; b0 < a->B; b0 += 64) total += read_lane(wave_scan(tiles_of_sequence(a, b0 + lane, unused[0], unused[1])), 63);
   // Tiles of a part: so many that there are no more parts than workers (one to a K/V head and sequence always fits)
   int per = (int)tiles_per_worker(a, total * a->Hkv);
   while (true) {
     long long n = read_lane(wave_scan((t + per - 1) / per), 63);
-    for (int b0 = 64; b0 < a->B; b0 += 64) n += read_lane(wave_scan((tiles_of_sequence(a, b0 + lane) + per - 1) / per), 63);
+    for (int b0 = 64; b0 < a->B; b0 += 64) n += read_lane(wave_scan((tiles_of_sequence(a, b0 + lane, unused[0], unused[1]) + per - 1) / per), 63);
     if (n * a->Hkv <= a->workers) break;
     per += per / 8 + 1;
   }
   u0 = 0;
   for (int b0 = 0; b0 < a->B; b0 += 64) {
-    if (b0 > 0) t = tiles_of_sequence(a, b0 + lane);
+    if (b0 > 0) t = tiles_of_sequence(a, b0 + lane, len, q_len);
     const int n = (t + per - 1) / per, upto = wave_scan(n * a->Hkv), all = read_lane(upto, 63);
     if (u >= 0 ? u < u0 + all : p.b < b0 + 64) {
       const int l = u >= 0 ? __builtin_ctzll(__ballot(upto > u - u0)) : p.b - b0;
       p.b = b0 + l;
-      p.n = read_lane(n, l);
+      p.n = read_lane(n, l); p.len = read_lane(len, l); p.q_len = read_lane(q_len, l);
       u0 += read_lane(upto, l) - p.n * a->Hkv;
       if (u >= 0) { p.index = divide(u - u0, a->by_Hkv); p.kvh = u - u0 - p.index * a->Hkv; }
       return true;
@@ -201,6 +204,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int slab = wave & 3, kind = wave >> 2;     // four waves move K and V of a slab each, eight one of the two
 
   // ---- this workgroup's tiles
+  const Hot h = hot_arguments();
+  Pages pages;
   Unit nxt;
   int left, row_base = 0;                          // tiles still to do; first query row
   long long slot = 2LL * blockIdx.x;               // of its partial results
@@ -208,11 +213,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const Args a = arguments();
     if constexpr (FLAT) {
       if (a->min_tiles == 0) {                     // a workgroup per (sequence, K/V head)
-        const int e = divide(blockIdx.x, a->by_Hkv);
-        open_unit<kTK>(nxt, e, blockIdx.x - e * a->Hkv, 0);
+        open_whole_unit<kTK>(nxt, pages, h, blockIdx.x);
         left = nxt.T;
       } else {
         left = open_share<kTK>(blockIdx.x, nxt);
+        pages.open(nxt.b);
       }
     } else {
       // The row tiles of a (sequence, K/V head, part) run one after the other on one XCD, whose L2 brings them K and V once
@@ -223,14 +228,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const int v = at / list * kNumXCDs + xcd, bh = v / a->cuts, rank = (at % list) * a->cuts + v % a->cuts;
         if (bh >= a->B * a->Hkv || rank >= a->row_tiles) return;
         const int b = divide(bh, a->by_Hkv);
-        open_unit<kTK>(nxt, b * a->row_tiles + a->row_tiles - 1 - rank, bh - b * a->Hkv, 0);
+        open_whole_unit<kTK>(nxt, pages, h, (b * a->row_tiles + a->row_tiles - 1 - rank) * a->Hkv + bh - b * a->Hkv);
         left = nxt.T;
       } else {
         const int g8 = divide(at, a->by_row_tiles), rt = at - g8 * a->row_tiles, u = g8 * kNumXCDs + xcd;
         Part p;
         int u0;
         if (!find_part(u, p, u0)) return;
-        open_unit<kTK>(nxt, p.b * a->row_tiles + rt, p.kvh, 0);
+        pages.open(p.b);
+        open_unit<kTK>(nxt, p.b * a->row_tiles + rt, p.kvh, 0, p.len, p.q_len);
         const int per = (nxt.T + p.n - 1) / p.n;
         nxt.i = p.index * per;
         left = min(per, nxt.T - nxt.i);
@@ -240,9 +246,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   if (left <= 0) return;
-  const Hot h = hot_arguments();
-  Pages pages;
-  pages.open(nxt.b);
   BlockRows block;
   block.open(nxt.b, nxt.kvh);
 
