@@ -204,3 +204,17 @@ def test_the_largest_scale(gpu_lib, dtype):
     """Weights of one and zero: the value of the key with the largest score."""
     s = attention_problem(34, dtype, 2, 4, 2, 64, 2, 16, [90, 40], None, False)
     check_attention(gpu_lib, s, dtype, scale=0.99e38)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("K,Hq", [(1, 2), (9, 4), (20, 4), (50, 4), (150, 4)])
+@pytest.mark.parametrize("page", [16, 32])
+def test_holes_in_long_tables(gpu_lib, dtype, K, Hq, page):
+    """Entries that are no pages on both sides of every 64th entry, alone and in runs, and behind the last one."""
+    s = attention_problem(35, dtype, 2, Hq, 2, 64, K, page, [3300, 1100], None, True)
+    for b, holes in ((0, [0, 1, 31, 62, 63, 64, 65, 66, 100, 127, 128, 192, 206]), (1, [33, 34, 35, 36, 63, 64])):
+        for e in holes:
+            if e < s["table"].shape[1]:
+                s["table"][b, e] = -1 if e % 2 else s["kp"].shape[0] + e
+    for mask in (dict(), dict(causal=True), dict(causal=True, window=1500, sinks=1100), dict(kv_splits=5)):
+        check_attention(gpu_lib, s, dtype, **mask)
