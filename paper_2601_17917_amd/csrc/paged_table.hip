@@ -170,7 +170,7 @@ hipError_t launch_paged_extend(const sdllm_paged_extend_params& p, int32_t* tabl
 }
 
 // ---- append: one lane per 16 bytes, source contiguous; a row's slot is one (cached) load.  Slots outside the pool are skipped.
-// Bound by HBM: 32 layers of 4 x 64 rows, 32 heads of 128, 268 MB in 48 us (5.5 TB/s).  The stores go past L2, which holds little of
+// Bound by HBM: 32 layers of 4 x 64 rows, 32 heads of 128, 268 MB in 47 us (5.7 TB/s).  The stores go past L2, which holds little of
 // this for whoever reads it: through it 53 us, and 6.8 instead of 6.2 for 32 layers of 4 x 32 rows of 8 heads.  Scalar decoding of
 // whole runs was no faster, eight accesses per lane were slower (75 us).
 struct PagedAppendArgs {
@@ -182,6 +182,7 @@ struct PagedAppendArgs {
 };
 constexpr int kPagedAppendUnroll = 4;
 
+template <bool LARGE>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   const unsigned l = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - l * (unsigned)a.parts;
   const u32x4* __restrict__ src = (blockIdx.y ? a.vb : a.kb) + (long long)l * a.block_layer16;
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
     slot[u] = -1;
     if (c >= a.chunks) continue;
     const unsigned row = a.row16.div(c), bh = a.K.div(row), t = row - bh * a.K.d, b = a.Hkv.div(bh), h = bh - b * a.Hkv.d;
-    v[u] = src[c];
+    v[u] = LARGE ? __builtin_nontemporal_load(src + c) : src[c];
     slot[u] = a.slots[(long long)b * a.K.d + t];
     at[u] = (h << 16) | (c - row * a.row16.d);
   }
@@ -221,7 +222,9 @@ hipError_t launch_paged_append(const sdllm_paged_append_params& p, void* k_pages
   a.block_layer16 = p.block_layer_stride ? p.block_layer_stride * elem / 16 : a.chunks;
   a.parts = (int)((a.chunks + 256 * kPagedAppendUnroll - 1) / (256 * kPagedAppendUnroll));
   const long long blocks = (long long)p.n_layers * a.parts;
-  hipLaunchKernelGGL(paged_append_kernel, dim3((unsigned)blocks, 2), dim3(256), 0, stream, a);
+  // Loads past L2, too, of what it could not hold: 47 us instead of 48 for the 268 MB above, but 7.4 instead of 6.2 for 32 MB.
+  if ((double)p.n_layers * a.chunks * 32 > 64e6) hipLaunchKernelGGL(paged_append_kernel<true>, dim3((unsigned)blocks, 2), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(paged_append_kernel<false>, dim3((unsigned)blocks, 2), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

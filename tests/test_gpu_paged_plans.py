@@ -218,3 +218,22 @@ def test_holes_in_long_tables(gpu_lib, dtype, K, Hq, page):
                 s["table"][b, e] = -1 if e % 2 else s["kp"].shape[0] + e
     for mask in (dict(), dict(causal=True), dict(causal=True, window=1500, sinks=1100), dict(kv_splits=5)):
         check_attention(gpu_lib, s, dtype, **mask)
+
+
+def test_append_of_many_rows(gpu_lib):
+    """More bytes than the caches hold are read another way; the layers one by one are not: the same pages."""
+    L, B, K, Hkv, D, page = 8, 4, 256, 32, 128, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(36)
+    k, v = (torch.randn((L, B, Hkv, K, D), generator=g, device="cuda").to(BF16) for _ in range(2))
+    n_pages = B * (K // page + 1) + 1
+    slots = torch.randperm(n_pages * page, generator=g, device="cuda")[:B * K].to(torch.int32).view(B, K)
+    slots[1, ::3] = -1
+    whole = [torch.zeros((L, n_pages, Hkv, page, D), dtype=BF16, device="cuda") for _ in range(2)]
+    parts = [torch.zeros_like(x) for x in whole]
+    gpu_lib.paged_kv_append(*whole, k, v, slots)
+    for l in range(L):
+        gpu_lib.paged_kv_append(parts[0][l:l + 1], parts[1][l:l + 1], k[l:l + 1], v[l:l + 1], slots)
+    assert torch.equal(whole[0], parts[0]) and torch.equal(whole[1], parts[1])
+    at = slots[0].long()
+    assert torch.equal(whole[0][:, at // page, :, at % page], k[:, 0].permute(2, 0, 1, 3)) and whole[1].abs().sum() > 0
