@@ -499,6 +499,57 @@ __device__ __forceinline__ void merge_waves(const Unit& u, int R0, int rows, int
   }
 }
 
+// Adds up the partial results first .. last of a row (slot(k): where the k-th lies, in rows), in groups of D / 4 lanes that take every
+// GROUPS-th each; then group 0 adds up the groups, in order.  All threads of the workgroup call it; the sum is group 0's.
+struct RowSum { f32x4 o; float m, l; };
+template <int D, int GROUPS, typename Slot>
+__device__ __forceinline__ RowSum add_up(Args a, int first, int last, Slot&& slot, bool exists) {
+  constexpr int TPR = D / 4;
+  const int grp = threadIdx.x / TPR % GROUPS, d = threadIdx.x % TPR * 4;
+  RowSum s{f32x4{0.f, 0.f, 0.f, 0.f}, kNegBig, 0.f};
+  auto add = [&](float mk, float lk, const f32x4& ov) {
+    const float up = fmaxf(s.m, mk), c0 = exp2_fast((s.m - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
+    s.o = s.o * c0 + ov * c1;
+    s.l = s.l * c0 + lk * c1;
+    s.m = up;
+  };
+  if (exists) {
+    int k = first + grp;
+    for (; k + 3 * GROUPS <= last; k += 4 * GROUPS) {          // four partial results' loads together
+      f32x4 ov[4]; float mk[4], lk[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const long long at = slot(k + u * GROUPS);
+        ov[u] = *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d);
+        mk[u] = a->ws_ml[2 * at]; lk[u] = a->ws_ml[2 * at + 1];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add(mk[u], lk[u], ov[u]);
+    }
+    for (; k <= last; k += GROUPS) {
+      const long long at = slot(k);
+      add(a->ws_ml[2 * at], a->ws_ml[2 * at + 1], *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d));
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    __shared__ f32x4 o_s[256];
+    __shared__ float m_s[256 / TPR], l_s[256 / TPR];
+    const int row0 = threadIdx.x / TPR - grp;                  // group 0 of the row
+    o_s[threadIdx.x] = s.o;
+    if (d == 0) { m_s[row0 + grp] = s.m; l_s[row0 + grp] = s.l; }
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+      for (int k = 1; k < GROUPS; ++k) add(m_s[row0 + k], l_s[row0 + k], o_s[(row0 + k) * TPR + d / 4]);
+    }
+  }
+  return s;
+}
+// Rows up to which each has a workgroup of its own for that: that many are on the chip at once, and what counts is the way through a
+// row's shares.  With more rows it is the number of workgroups.  (32 query heads, one row each, over 32768 keys: 35 us with the
+// attention itself, 67 with all rows in 128 workgroups; 28 heads of 32 rows for 8 sequences of 4096 keys: 55 and 48.)
+constexpr int kMergeAlone = 8 * kNumCUs;
+
 // Kernels: bf16 by query rows per (sequence, K/V head), up to 32 (stream) and more (tile); fp32
 size_t paged_stream_workspace_bytes(const sdllm_paged_attn_params& p, bool with_block);
 hipError_t launch_paged_stream(const sdllm_paged_attn_params& p, PagedArgs& a, void* workspace, hipStream_t stream);

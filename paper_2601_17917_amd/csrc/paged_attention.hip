@@ -4,15 +4,11 @@
 
 namespace sdllm {
 
-// Merges the shares of every output row that several workers walked, in the order of the tiles.  GROUPS groups of D / 4 lanes take
-// every so many-th share of a row, then one adds up the groups, in order: one group per row where there are many rows (a
-// workgroup then merges several), else a workgroup per row.
+// Merges the shares of every output row that several workers walked, in the order of the tiles: GROUPS groups of D / 4 lanes per row
 template <typename T, int D, int TK, int GROUPS>
 __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
   const Args a = arguments();
   constexpr int TPR = D / 4, RPW = 256 / (TPR * GROUPS);
-  __shared__ f32x4 o_s[GROUPS > 1 ? GROUPS : 1][TPR];
-  __shared__ float m_s[GROUPS], l_s[GROUPS];
   const int grp = threadIdx.x / TPR % GROUPS, d = threadIdx.x % TPR * 4;
   // the rows of a workgroup: of one (sequence, K/V head, row tile)
   const int per_tile = (a->tile_rows + RPW - 1) / RPW;
@@ -37,43 +33,11 @@ __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
   if (w0 == w1) return;                            // written by its worker
   const int q_len = min(max(a->q_lens ? a->q_lens[b] : a->K, 0), a->K);
   const bool exists = row < a->tile_rows && R < q_len * a->g;
-  float M = kNegBig, l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  auto add = [&](float mk, float lk, const f32x4& ov) {
-    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
-    acc = acc * c0 + ov * c1;
-    l = l * c0 + lk * c1;
-    M = up;
-  };
-  if (exists) {
-    // a unit is its worker's first one unless the worker began before it
-    auto slot = [&](int w) { return ((long long)w * 2 + (start > w * per ? 1 : 0)) * a->tile_rows + row; };
-    int w = w0 + grp;
-    for (; w + 3 * GROUPS <= w1; w += 4 * GROUPS) {            // four shares' loads together
-      f32x4 ov[4]; float mk[4], lk[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const long long at = slot(w + u * GROUPS);
-        ov[u] = *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d);
-        mk[u] = a->ws_ml[2 * at]; lk[u] = a->ws_ml[2 * at + 1];
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) add(mk[u], lk[u], ov[u]);
-    }
-    for (; w <= w1; w += GROUPS) {
-      const long long at = slot(w);
-      add(a->ws_ml[2 * at], a->ws_ml[2 * at + 1], *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d));
-    }
-  }
-  if constexpr (GROUPS > 1) {
-    o_s[grp][threadIdx.x % TPR] = acc;
-    if (d == 0) { m_s[grp] = M; l_s[grp] = l; }
-    __syncthreads();
-    if (grp != 0) return;
-#pragma unroll
-    for (int k = 1; k < GROUPS; ++k) add(m_s[k], l_s[k], o_s[k][threadIdx.x % TPR]);
-  }
-  if (!exists) return;
+  // a unit is its worker's first one unless the worker began before it
+  const RowSum sum = add_up<D, GROUPS>(a, w0, w1, [&](int w) { return ((long long)w * 2 + (start > w * per ? 1 : 0)) * a->tile_rows + row; }, exists);
+  if (grp != 0 || !exists) return;
+  const f32x4 acc = sum.o;
+  const float l = sum.l;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
   T* out = (T*)a->out + b * a->o_st[0] + h * a->o_st[1] + r * a->o_st[2] + d;
@@ -86,11 +50,6 @@ __global__ __launch_bounds__(256) void shares_merge_kernel(PagedArgs) {
     *reinterpret_cast<uint2*>(out) = w2;
   }
 }
-
-// Rows up to which each has a workgroup of its own: that many are on the chip at once, and what counts is the way through a row's
-// shares.  With more rows it is the number of workgroups.  (32 query heads, one row each, over 32768 keys: 35 us with the attention
-// itself, 67 with all rows in 128 workgroups; 28 heads of 32 rows for 8 sequences of 4096 keys: 55 and 48.)
-constexpr int kMergeAlone = 8 * kNumCUs;
 
 template <typename T, int D, int TK>
 static void launch_merge(const PagedArgs& a, hipStream_t stream) {

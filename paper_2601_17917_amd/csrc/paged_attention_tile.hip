@@ -454,48 +454,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// Merges the parts of a row that a row tile's workgroups left, in the order of the keys: D / 4 lanes per row
-template <int D>
+// Merges the parts of a row that a row tile's workgroups left, in the order of the keys: GROUPS groups of D / 4 lanes per row
+template <int D, int GROUPS>
 __global__ __launch_bounds__(256) void paged_parts_merge_kernel(PagedArgs) {
   const Args a = arguments();
-  constexpr int TPR = D / 4, RPB = 256 / TPR;
+  constexpr int TPR = D / 4, RPB = 256 / (TPR * GROUPS);
   const int per_unit = (a->R + RPB - 1) / RPB, unit = blockIdx.x / (unsigned)per_unit;
   Part p;
   p.b = divide(unit, a->by_Hkv);
   const int b = p.b, kvh = unit - b * a->Hkv;
   int u0;
   find_part(-1, p, u0);
-  const int R = (blockIdx.x - unit * per_unit) * RPB + threadIdx.x / TPR, rt = divide(R, a->by_tile_rows);
-  const Seen s = entry_seen<kTK>(a, a->lens[b], a->q_lens ? a->q_lens[b] : a->K, rt);
-  if (R >= s.q_len * a->g) return;
-  const int T = tiles_to_do(a, s, rt), per = (T + p.n - 1) / p.n, n = (T + per - 1) / per;
-  if (n == 1) return;                              // written by its workgroup
-  const int d = (threadIdx.x % TPR) * 4;
-  float M = kNegBig, l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  auto slot = [&](int k) { return (u0 + k * a->Hkv + kvh) * (long long)a->R + R; };
-  auto add = [&](float mk, float lk, const f32x4& ov) {
-    const float up = fmaxf(M, mk), c0 = exp2_fast((M - up) * a->scale_log2), c1 = exp2_fast((mk - up) * a->scale_log2);
-    acc = acc * c0 + ov * c1;
-    l = l * c0 + lk * c1;
-    M = up;
-  };
-  int k = 0;
-  for (; k + 4 <= n; k += 4) {                     // four parts' loads together
-    f32x4 ov[4]; float mk[4], lk[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const long long at = slot(k + x);
-      ov[x] = *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d);
-      mk[x] = a->ws_ml[2 * at]; lk[x] = a->ws_ml[2 * at + 1];
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x) add(mk[x], lk[x], ov[x]);
+  const int R = (blockIdx.x - unit * per_unit) * RPB + threadIdx.x / (TPR * GROUPS), rt = divide(R, a->by_tile_rows);
+  const Seen s = entry_seen<kTK>(a, p.len, p.q_len, rt);
+  int n = 0;                                       // parts; of one, the workgroup has written the output
+  if (R < s.q_len * a->g) {
+    const int T = tiles_to_do(a, s, rt), per = (T + p.n - 1) / p.n;
+    n = (T + per - 1) / per;
   }
-  for (; k < n; ++k) {
-    const long long at = slot(k);
-    add(a->ws_ml[2 * at], a->ws_ml[2 * at + 1], *reinterpret_cast<const f32x4*>(a->ws_o + at * D + d));
-  }
+  const RowSum sum = add_up<D, GROUPS>(a, 0, n - 1, [&](int k) { return (u0 + k * a->Hkv + kvh) * (long long)a->R + R; }, n > 1);
+  if (n <= 1 || threadIdx.x / TPR % GROUPS != 0) return;
+  const int d = threadIdx.x % TPR * 4;
+  const f32x4 acc = sum.o;
+  const float l = sum.l;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   const int r = divide(R, a->by_g), h = kvh * a->g + R - r * a->g;
   uint2 w2;
@@ -593,10 +574,18 @@ hipError_t launch_paged_tile(const sdllm_paged_attn_params& p, PagedArgs& a, voi
   hipError_t e = p.D == 128 ? launch_tile_d<128>(a, pl, (unsigned)grid, stream) : launch_tile_d<64>(a, pl, (unsigned)grid, stream);
   if (e != hipSuccess || pl.shares.min_tiles == 0) return e;
   if (pl.flat) return launch_shares_merge(a, p.dtype, p.D, kTK, stream);
-  const int rpb = 256 / (p.D / 4);
-  const unsigned blocks = (unsigned)(units * ((a.R + rpb - 1) / rpb));
-  if (p.D == 128) hipLaunchKernelGGL(paged_parts_merge_kernel<128>, dim3(blocks), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(paged_parts_merge_kernel<64>, dim3(blocks), dim3(256), 0, stream, a);
+  const int all = 256 / (p.D / 4);
+  // a workgroup per row for few rows of many parts (us, with the attention, a workgroup per row and not: 320 rows, 63 parts 17 and 22; 896
+  // rows, 63 parts 28 and 31; 896 rows, 5 parts 16.5 and 15.3; 1792 rows, 32 parts 29.7 and 29.1)
+  const bool alone = units * a.R <= kMergeAlone / 2 && pl.slots >= 16 * units;
+  const dim3 grid_m((unsigned)(units * (alone ? a.R : (a.R + all - 1) / all)));
+  if (p.D == 128) {
+    if (alone) hipLaunchKernelGGL((paged_parts_merge_kernel<128, 8>), grid_m, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((paged_parts_merge_kernel<128, 1>), grid_m, dim3(256), 0, stream, a);
+  } else {
+    if (alone) hipLaunchKernelGGL((paged_parts_merge_kernel<64, 16>), grid_m, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((paged_parts_merge_kernel<64, 1>), grid_m, dim3(256), 0, stream, a);
+  }
   return hipGetLastError();
 }
 
