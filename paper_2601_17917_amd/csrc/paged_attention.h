@@ -259,11 +259,20 @@ template <int D> struct Slab {
   static constexpr int IPT = 16 / RPI;             // transfers per slab
   static constexpr int R256 = 16 / CPR;            // rows per 256 bytes
   static constexpr int ROWB = D * 2, BYTES = 16 * ROWB;
+  // where chunk c of row r lies in its LDS row (and which chunk lies at c)
+  __host__ __device__ static constexpr int at(bool v, int r, int c) { return c ^ (v ? 2 * ((r / R256) % (CPR / 2)) : (r / R256) % CPR); }
   // byte within the source of the lane's chunk of transfer 0, and the bits of it that transfer j flips (less j KiB, dma_slab)
   __device__ static unsigned lane_offset(bool v) {
     const int lane = fresh_lane(), r = lane / CPR, c = lane % CPR;
-    return r * ROWB + ((c ^ (v ? 2 * ((r / R256) % (CPR / 2)) : (r / R256) % CPR)) << 4);
+    return r * ROWB + (at(v, r, c) << 4);
   }
+  // The same for rows `stride` bytes apart, transfer j.  The hardware adds it to a scalar address as an unsigned number of 32 bits, so it
+  // must not be negative: transfer j begins with row RPI j, which is j KiB in or more if rows do not overlap (RPI ROWB = 1 KiB).
+  __host__ __device__ static constexpr unsigned strided_offset(bool v, int lane, int j, unsigned stride) {
+    const int r = RPI * j + lane / CPR;
+    return r * stride + (at(v, r, lane % CPR) << 4) - 1024 * j;
+  }
+  __host__ __device__ static constexpr bool strided(long long stride) { return stride >= ROWB && stride < (1 << 27); }
   __device__ static constexpr unsigned flips(bool v, int j) { return v ? (D == 128 ? 128 * (j & 1) : 0) : 64 * j; }
   __device__ static __forceinline__ void offsets(bool v, unsigned (&off)[4]) {
     const unsigned g = lane_offset(v);
@@ -284,24 +293,21 @@ __device__ __forceinline__ void move_slab(unsigned lds, const unsigned char* src
 template <int D, bool ONCE, bool V>
 __device__ __forceinline__ void move_strided(unsigned lds, const unsigned char* src, unsigned stride) {
   using S = Slab<D>;
-  const int lane = fresh_lane(), c = lane % S::CPR;
+  const int lane = fresh_lane();
   unsigned off[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = S::RPI * (j < S::IPT ? j : 0) + lane / S::CPR;
-    off[j] = r * stride + ((c ^ (V ? 2 * ((r / S::R256) % (S::CPR / 2)) : (r / S::R256) % S::CPR)) << 4) - 1024 * (j < S::IPT ? j : 0);
-  }
+  for (int j = 0; j < 4; ++j) off[j] = S::strided_offset(V, lane, j < S::IPT ? j : 0, stride);
   dma_slab<S::IPT, ONCE>(lds, uniform_ptr(src), off);
 }
 // The block's rows of a (sequence, K/V head)
-struct BlockRows {
+template <int D> struct BlockRows {
   const unsigned char *k, *v;                      // of row 0
-  unsigned k_stride, v_stride;                     // bytes between rows; 0: no block, or too far apart for an offset of 32 bits
+  unsigned k_stride, v_stride;                     // bytes between rows; 0: no block, or rows that only move_rows can address
   __device__ __forceinline__ void open(int b, int kvh) {
     const Args a = arguments();
     k_stride = v_stride = 0;
     k = v = nullptr;
-    if (a->kb == nullptr || a->kb_st[2] >= (1 << 26) || a->vb_st[2] >= (1 << 26)) return;
+    if (a->kb == nullptr || !Slab<D>::strided(2 * a->kb_st[2]) || !Slab<D>::strided(2 * a->vb_st[2])) return;
     k = (const unsigned char*)a->kb + 2 * (b * a->kb_st[0] + kvh * a->kb_st[1]);
     v = (const unsigned char*)a->vb + 2 * (b * a->vb_st[0] + kvh * a->vb_st[1]);
     k_stride = (unsigned)(2 * a->kb_st[2]); v_stride = (unsigned)(2 * a->vb_st[2]);
@@ -335,7 +341,7 @@ __device__ __forceinline__ void move_rows(const Seen& s, int b, int kvh, int k, 
 #pragma unroll 1
   for (int t = 0; t < S::IPT; ++t) {
     const int r = S::RPI * t + lane / S::CPR;
-    const int at = (c ^ (V ? 2 * ((r / S::R256) % (S::CPR / 2)) : (r / S::R256) % S::CPR)) << 4;
+    const int at = S::at(V, r, c) << 4;
     if ((bits >> r) & 1) dma16_vaddr<ONCE>(lds + 1024 * t, (k + r < s.n ? page_row + r * S::ROWB : block + 2 * r * st) + at);
   }
 }

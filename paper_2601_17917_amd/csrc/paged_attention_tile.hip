@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   if (left <= 0) return;
-  BlockRows block;
+  BlockRows<D> block;
   block.open(nxt.b, nxt.kvh);
 
   // LDS addresses of the lane's operands of slice 0 / d block 0 in stage 0; the others flip bits of them
