@@ -28,7 +28,8 @@ extern "C" {
 /* ---------------------------------------------------------------------------------------
  * Block tables and slots from request lengths.  free_pages[0 .. n_free) is a stack of page ids (top at n_free - 1).
  *  1. In batch order every sequence with release[b] != 0 pushes the pages of its kv_lens[b] rows, in table order, and its
- *     length becomes 0 (a finished request makes room for the next one in its batch slot).
+ *     length becomes 0 (a finished request makes room for the next one in its batch slot).  Entries outside [0, n_pages) are no
+ *     pages and are not pushed: a page that was given back before (behind a window) and its entry set to -1 does not come back again.
  *  2. Sequence b asks for n = clamp(new_lens[b], 0, K) rows (new_lens NULL: K; do_append[b] == 0: none), that is for
  *     ceil((len + n) / page_size) - ceil(len / page_size) pages.  In batch order the pages are popped off the stack, top first,
  *     into the table entries behind the ones in use.  A sequence gets all of its rows or none: none if len + n exceeds

@@ -4,7 +4,8 @@ import numpy as np
 
 def paged_extend(block_table, kv_lens, free_pages, n_free, page_size, K, new_lens=None, do_append=None, release=None):
     """One sequence after the other, one page after the other.  Returns (block_table, kv_lens, free_pages, n_free, slots, granted)
-    as new arrays; `need so far` counts the sequences that were refused for want of pages, too."""
+    as new arrays; `need so far` counts the sequences that were refused for want of pages, too.  Entries of a released sequence that
+    are no pages of the pool do not go on the stack."""
     table, lens, stack = block_table.copy(), [int(x) for x in kv_lens], free_pages.copy()
     B, max_pages = table.shape
     n_pages, top = len(stack), min(max(int(n_free), 0), len(free_pages))
@@ -14,7 +15,7 @@ def paged_extend(block_table, kv_lens, free_pages, n_free, page_size, K, new_len
         for b in range(B):
             if release[b]:
                 for e in range(pages(lens[b])):
-                    if top < n_pages:
+                    if 0 <= block_table[b, e] < n_pages and top < n_pages:
                         stack[top] = block_table[b, e]
                         top += 1
                 lens[b] = 0

@@ -1,8 +1,8 @@
 // Block tables and slots of a paged K/V cache (sdllm_paged_extend) and the append of K/V rows into their slots
 // (sdllm_paged_kv_append).
 //
-// Extend is three prefix sums over the batch -- pages given back, pages needed, pages granted so far -- and a fill of the tables
-// and slots they decide.  It moves a few bytes per row, so what it costs is launches and dependent round trips: one workgroup
+// Extend is prefix sums over the batch -- table entries of released sequences, which of them are pages, pages needed, pages granted
+// so far -- and a fill of the tables and slots they decide.  It moves a few bytes per row, so what it costs is launches and dependent round trips: one workgroup
 // does the scans and, where there are few rows, the fill behind them; many rows are filled by a second launch over the chip.
 // Measured: 8 sequences of one row 2.0 us in the kernel; 64 of up to 2048 rows, a third of them new, 6.0 + 3.8 us.
 #include "paged_common.h"
@@ -16,7 +16,6 @@ struct ExtendArgs {
   int B, K, shift, max_pages, n_pages;
 };
 
-constexpr int kReleaseLoads = 8;              // table entries that a lane has in flight
 constexpr int kExtendOneLaunch = 16384;       // rows of the batch up to which the scanning workgroup fills them itself
 
 // Inclusive sum over the workgroup of one value per thread; `total` receives the sum of all.  NT threads, 64-wide waves.
@@ -62,30 +61,50 @@ __global__ __launch_bounds__(NT) void paged_extend_scan_kernel(ExtendArgs a) {
   int avail = min(max(a.n_free[0], 0), a.n_pages);
 
   if (a.release != nullptr) {                  // pages that come back, in batch order
+    constexpr int kReleaseLoads = NT == 64 ? 8 : 4;                   // table entries that a lane has in flight
     for (int b0 = 0; b0 < a.B; b0 += NT) {
       const int b = b0 + tid;
-      int n = 0;
+      int held = 0;
       if (b < a.B) {
         const int len = a.lens[b];                 // asked for at once with the flag
-        n = a.release[b] != 0 ? (min(max(len, 0), cap) + mask) >> a.shift : 0;
+        held = a.release[b] != 0 ? (min(max(len, 0), cap) + mask) >> a.shift : 0;
       }
-      int total;
-      const int upto = block_scan<NT>(n, wave_sums, total);
-      __syncthreads();                         // the previous chunk's entries are read
-      s_first[tid] = avail + upto - n; s_n[tid] = n;
+      // The entries of the chunk's released sequences, one row after the other; s_first: where a sequence's begin
+      int all;
+      const int upto = block_scan<NT>(held, wave_sums, all);
+      s_first[tid] = upto - held;
       __syncthreads();
-      for (int i = tid >> 6; i < min(NT, a.B - b0); i += NT / 64)       // a wave per sequence
-        for (int e0 = tid & 63; e0 < s_n[i]; e0 += 64 * kReleaseLoads) {
-          const int32_t* row = a.table + (long long)(b0 + i) * a.max_pages;
-          const int first = s_first[i], n = min(s_n[i], a.n_pages - first);
-          int page[kReleaseLoads];
+      auto sequence_of = [&](int e) {              // the last one that begins at e or before it: those without entries are in front of it
+        int s = 0;
 #pragma unroll
-          for (int u = 0; u < kReleaseLoads; ++u) page[u] = row[min(e0 + 64 * u, s_n[i] - 1)];
+        for (int step = NT / 2; step > 0; step >>= 1)
+          if (s_first[s + step] <= e) s += step;
+        return s;
+      };
+      for (int e0 = 0; e0 < all; e0 += NT * kReleaseLoads) {
+        const int e = e0 + tid * kReleaseLoads, n = min(kReleaseLoads, all - e);
+        int id[kReleaseLoads];
+        int s = 0, begin = 0, end = 0;             // entries of sequence s
 #pragma unroll
-          for (int u = 0; u < kReleaseLoads; ++u)
-            if (e0 + 64 * u < n) a.free_pages[first + e0 + 64 * u] = page[u];
+        for (int u = 0; u < kReleaseLoads; ++u) {
+          id[u] = -1;
+          if (u >= n) continue;
+          if (e + u >= end) {
+            s = sequence_of(e + u);
+            begin = s_first[s];
+            end = s + 1 < NT ? s_first[s + 1] : all;
+          }
+          id[u] = a.table[(long long)(b0 + s) * a.max_pages + e + u - begin];
         }
-      avail = min(avail + total, a.n_pages);
+        int pages = 0, got;                        // entries that are no pages stay behind
+#pragma unroll
+        for (int u = 0; u < kReleaseLoads; ++u) pages += (unsigned)id[u] < (unsigned)a.n_pages;
+        int to = avail + block_scan<NT>(pages, wave_sums, got) - pages;
+#pragma unroll
+        for (int u = 0; u < kReleaseLoads; ++u)
+          if ((unsigned)id[u] < (unsigned)a.n_pages && to < a.n_pages) a.free_pages[to++] = id[u];
+        avail = min(avail + got, a.n_pages);
+      }
     }
     __syncthreads();                           // pushed entries may be popped below
   }
