@@ -588,12 +588,18 @@ def _on_current_device(*tensors):
 
 
 def _new(shape, dtype, device, stream):
-    """A tensor that the call makes; one that another stream than the current one works on is not handed out again before that
-    stream is done with it."""
+    """A tensor that the call makes for the stream it works on (None: the current one).  Its memory is that stream's: a block of the
+    current stream's may still be in use by work queued there.  The current stream, on which the caller goes on with a result, is
+    made known to the allocator, too, so that the block is not handed out again before that stream is done with it."""
     import torch
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None and stream != torch.cuda.current_stream(device):
-        t.record_stream(stream)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if stream == current:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
     return t
 
 
