@@ -236,6 +236,22 @@ def _require(t, name, dtype=None):
         raise SdllmError(ERR_INVALID_ARG, f"{name} must have dtype {dtype}, has {t.dtype}")
 
 
+def _new(shape, dtype, device, stream):
+    """A tensor that the call makes for the stream it works on (None: the current one).  Its memory is that stream's: a block of the
+    current stream's may still be in use by work queued there.  The current stream, on which the caller goes on with a result, is
+    made known to the allocator, too, so that the block is not handed out again before that stream is done with it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if stream == current:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def init():
     """sdllm_init on the current device: every kernel opt-in done, so that later calls only launch."""
     _check(load_library().sdllm_init())
@@ -313,12 +329,12 @@ def bind_block_attention(q_block, q_suffix, k_cache, v_cache, k_block, v_block, 
     _require(keep_idx, "keep_idx", torch.int32)
     p = attn_params(_dtype_code(q_block), B, Hq, Hkv, D, prefix_len, cap, K, S, n_keep, scale, kv_splits)
     if out is None:
-        out = torch.empty((B, Hq, K + n_keep, D), dtype=dtype, device=q_block.device)
+        out = _new((B, Hq, K + n_keep, D), dtype, q_block.device, stream)
     else:
         _require(out, "out", dtype)
     need = attention_workspace_bytes(p)
     if need and workspace is None:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q_block.device)
+        workspace = _new((need,), torch.uint8, q_block.device, stream)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     kidx = keep_idx if n_keep else None
     args = (ctypes.byref(p), _ptr(q_block), _ptr(q_suffix), _ptr(k_cache), _ptr(v_cache), _ptr(k_block), _ptr(v_block),
@@ -360,15 +376,15 @@ def bind_confidence_unmask(logits, tokens, masked, tau0: float, alpha: float, V:
     _require(confidence, "confidence", torch.float32)
     _require(eos_seen, "eos_seen", torch.uint8)
     if n_committed is None:
-        n_committed = torch.empty((B,), dtype=torch.int32, device=logits.device)
+        n_committed = _new((B,), torch.int32, logits.device, stream)
     if block_done is None:
-        block_done = torch.empty((B,), dtype=torch.uint8, device=logits.device)
+        block_done = _new((B,), torch.uint8, logits.device, stream)
     _require(n_committed, "n_committed", torch.int32)
     _require(block_done, "block_done", torch.uint8)
     p = unmask_params(_dtype_code(logits), B, K, V, ld, tau0, alpha, r_extra_masked, r_extra_total, eos_id, tau_eos)
     need = unmask_workspace_bytes(p)
     if workspace is None:
-        workspace = torch.empty((max(need, 16),), dtype=torch.uint8, device=logits.device)
+        workspace = _new((max(need, 16),), torch.uint8, logits.device, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     args = (ctypes.byref(p), _ptr(logits), _ptr(tokens), _ptr(masked), _ptr(confidence), _ptr(n_committed),
             _ptr(block_done), _ptr(eos_seen), _ptr(workspace), ws_bytes, _stream(stream))
@@ -399,9 +415,9 @@ def bind_confidence_unmask_noalloc(logits, tokens, masked, tau0: float, alpha: f
     _require(confidence, "confidence", torch.float32)
     _require(eos_seen, "eos_seen", torch.uint8)
     if n_committed is None:
-        n_committed = torch.empty((B,), dtype=torch.int32, device=logits.device)
+        n_committed = _new((B,), torch.int32, logits.device, stream)
     if block_done is None:
-        block_done = torch.empty((B,), dtype=torch.uint8, device=logits.device)
+        block_done = _new((B,), torch.uint8, logits.device, stream)
     _require(n_committed, "n_committed", torch.int32)
     _require(block_done, "block_done", torch.uint8)
     p = unmask_params(_dtype_code(logits), B, K, V, ld, tau0, alpha, r_extra_masked, r_extra_total, eos_id, tau_eos)
@@ -439,7 +455,7 @@ def lm_head_pack_weight(weight, stream=None) -> PackedLmWeight:
     if weight.dtype != torch.bfloat16 or not weight.is_cuda or weight.dim() != 2 or weight.stride(1) != 1:
         raise ValueError("lm_head_pack_weight: need a bfloat16 device tensor [V, Hd] with contiguous rows")
     V, Hd = weight.shape
-    data = torch.empty((lm_head_packed_weight_bytes(V, Hd) // 2,), dtype=torch.bfloat16, device=weight.device)
+    data = _new((lm_head_packed_weight_bytes(V, Hd) // 2,), torch.bfloat16, weight.device, stream)
     _check(load_library().sdllm_lm_head_pack_weight(V, Hd, weight.stride(0), _ptr(weight), _ptr(data), _stream(stream)))
     return PackedLmWeight(data, V, Hd)
 
@@ -489,16 +505,16 @@ def bind_lm_head_unmask(hidden, weight, tokens, masked, tau0: float, alpha: floa
     _require(confidence, "confidence", torch.float32)
     _require(eos_seen, "eos_seen", torch.uint8)
     if n_committed is None:
-        n_committed = torch.empty((B,), dtype=torch.int32, device=hidden.device)
+        n_committed = _new((B,), torch.int32, hidden.device, stream)
     if block_done is None:
-        block_done = torch.empty((B,), dtype=torch.uint8, device=hidden.device)
+        block_done = _new((B,), torch.uint8, hidden.device, stream)
     _require(n_committed, "n_committed", torch.int32)
     _require(block_done, "block_done", torch.uint8)
     p = lm_head_params(B, K, V, Hd, hidden.stride(1), ld_w, tau0, alpha, r_extra_masked, r_extra_total,
                        eos_id, tau_eos, 1 if packed else 0)
     need = lm_head_unmask_workspace_bytes(p)
     if workspace is None:
-        workspace = torch.empty((max(need, 16),), dtype=torch.uint8, device=hidden.device)
+        workspace = _new((max(need, 16),), torch.uint8, hidden.device, stream)
     ws_bytes = workspace.numel() * workspace.element_size()
     args = (ctypes.byref(p), _ptr(hidden), _ptr(weight), _ptr(tokens), _ptr(masked), _ptr(confidence),
             _ptr(n_committed), _ptr(block_done), _ptr(eos_seen), _ptr(workspace), ws_bytes, _stream(stream))
@@ -585,22 +601,6 @@ def _on_current_device(*tensors):
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise SdllmError(ERR_INVALID_ARG, f"a tensor is on {t.device}, the current device is cuda:{dev}")
-
-
-def _new(shape, dtype, device, stream):
-    """A tensor that the call makes for the stream it works on (None: the current one).  Its memory is that stream's: a block of the
-    current stream's may still be in use by work queued there.  The current stream, on which the caller goes on with a result, is
-    made known to the allocator, too, so that the block is not handed out again before that stream is done with it."""
-    import torch
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    current = torch.cuda.current_stream(device)
-    if stream == current:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(current)
-    return t
 
 
 def _shaped(t, name, shape, dtype):

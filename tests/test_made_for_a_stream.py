@@ -91,3 +91,36 @@ def test_results_and_workspaces_of_the_paged_calls(gpu_lib, what):
     workspace = call._keep[2] if len(call._keep) > 2 else None
     assert (workspace is not None) == (what in ("attention", "extend in two launches"))
     assert all(owner(t) == side.cuda_stream for t in (*results, workspace) if t is not None)
+
+
+@pytest.mark.gpu
+def test_results_and_workspaces_of_the_step(gpu_lib):
+    """The calls of a decode step over the dense cache: same results, and all that they make belongs to the stream they work on."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(53)
+    draw = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+    B, K, V, Hd = 2, 32, 1000, 256
+    q, k, cache = draw(B, 4, K, 128), draw(B, 4, K, 128), draw(B, 4, 4096, 128)
+    none = (None, None, None)
+    logits, hidden, weight = draw(B, K, V), draw(B, K, Hd), draw(V, Hd)
+    state = lambda: (torch.zeros((B, K), dtype=torch.int32, device="cuda"), torch.ones((B, K), dtype=torch.uint8, device="cuda"))
+    calls = {"attention": lambda st, **kw: gpu_lib.bind_block_attention(q, None, cache, cache, k, k, *none, 4096, **kw),
+             "unmask": lambda st, **kw: gpu_lib.bind_confidence_unmask(logits, *st, 0.9, 0.5, **kw),
+             "unmask, no workspace": lambda st, **kw: gpu_lib.bind_confidence_unmask_noalloc(logits, *st, 0.9, 0.5, **kw),
+             "projection": lambda st, **kw: gpu_lib.bind_lm_head_unmask(hidden, weight, *st, 0.9, 0.5, **kw)}
+    side = torch.cuda.Stream()
+    for name, bind in calls.items():
+        first, again = state(), state()
+        call = bind(first)
+        want = call()
+        torch.cuda.synchronize()
+        call = bind(again, stream=side)
+        got = call()
+        torch.cuda.synchronize()
+        want, got = (x if isinstance(x, tuple) else (x,) for x in (want, got))
+        assert all(torch.equal(x, y) for x, y in zip((*first, *want), (*again, *got))), name
+        workspace = call._keep[-1] if name != "unmask, no workspace" else None
+        assert all(owner(t) == side.cuda_stream for t in (*got, workspace) if t is not None), name
+    packed = gpu_lib.lm_head_pack_weight(weight, stream=side)
+    torch.cuda.synchronize()
+    assert owner(packed.data) == side.cuda_stream and torch.equal(packed.data, gpu_lib.lm_head_pack_weight(weight).data)
