@@ -152,8 +152,8 @@ int sdllm_paged_kv_append(const sdllm_paged_append_params* p,
  *   max_kv_len      upper bound of kv_lens, <= max_pages * page_size: the launch plan is made for it (the lengths themselves are
  *                   device data); max_kv_len + K <= 2^30
  *   scale           softmax scale, at most 1e38; <= 0 selects 1/sqrt(D)
- *   kv_splits       0 = choose automatically; n >= 1: a sequence of max_kv_len keys is cut into about n parts, if the batch is not so
- *                   large that parts gain nothing
+ *   kv_splits       0 = choose automatically; n >= 1: a sequence of max_kv_len keys is cut into about n parts, unless
+ *                   batch or sequences are so large that keys are not shared out
  *   *_stride        as for sdllm_qk_norm_rope; the rows of q and of the block may overlap
  * Out of range: kv_lens is clamped to [0, max_kv_len], q_lens to [0, K]; the keys of a page id outside [0, n_pages) are hidden
  * (a page that has left the window may be given back and its entry set to -1).

@@ -108,7 +108,7 @@ __device__ __forceinline__ int tiles_to_do(Args a, const Seen& s, int rt) {
   // rows that see nothing are a tile of their own: they are zero
   return rt * a->tile_rows < s.q_len * a->g ? max(s.tiles, 1) : 0;
 }
-// Key tiles of entries e0 .. e0 + 63, one per lane, and their sums up to the lane
+// Key tiles of entries e0 .. e0 + 63, one per lane, and their sums up to the lane (below 2^31 where keys are shared out, plan_shares)
 struct Entries { int n, q_len, tiles, upto; };
 template <int TK>
 __device__ __forceinline__ Entries entries(Args a, int e0) {

@@ -93,8 +93,11 @@ SharePlan plan_shares(const sdllm_paged_attn_params& p, bool with_block, int til
   const long long units = (long long)p.B * p.Hkv * row_tiles, tiles = paged_most_tiles(p, with_block, tile_rows, TK);
   const long long per = p.kv_splits > 0 ? (tiles + p.kv_splits - 1) / p.kv_splits : min_tiles;
   // A worker per unit where a unit is one share anyway, where the units go round all workers several times, and where finding the
-  // shares (a walk over the batch's lengths) or the merge's grid would get long
-  if (p.kv_splits == 1 || tiles <= per || units * tile_rows >= (1 << 23) || (long long)p.B * row_tiles > 2048 || (p.kv_splits == 0 && units >= 2LL * at_once))
+  // shares (a walk over the batch's lengths) or the merge's grid would get long; and where the tiles of the 64 entries that are added up
+  // at a time (entries) might not fit 32 bits
+  const long long entries = (long long)p.B * row_tiles;
+  if (p.kv_splits == 1 || tiles <= per || units * tile_rows >= (1 << 23) || entries > 2048 || (p.kv_splits == 0 && units >= 2LL * at_once) ||
+      (entries < 64 ? entries : 64) * tiles >= (1LL << 31))
     return SharePlan{(int)units, 0};
   const long long w = (units * tiles + per - 1) / per, most = p.kv_splits > 0 ? 1 << 18 : at_once;
   return SharePlan{(int)(w < most ? w : most), (int)per};
