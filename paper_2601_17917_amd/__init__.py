@@ -594,10 +594,12 @@ def bind_rope_gathered(x_block, x_suffix, keep_idx, pos0: int, theta_base: float
 
 # ---------------------------------------------------------------------------------------------
 # The paged cache (include/sdllm_paged.h).
-def _on_current_device(*tensors):
-    """All tensors on the device whose stream the call is enqueued on: a kernel launched there may not reach others."""
+def _on_current_device(stream, *tensors):
+    """The stream (None: the current one) and all tensors on the current device: a kernel launched there may not reach others."""
     import torch
     dev = torch.cuda.current_device()
+    if stream is not None and stream.device.index != dev:
+        raise SdllmError(ERR_INVALID_ARG, f"the stream is on {stream.device}, the current device is cuda:{dev}")
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise SdllmError(ERR_INVALID_ARG, f"a tensor is on {t.device}, the current device is cuda:{dev}")
@@ -669,7 +671,7 @@ def bind_paged_extend(block_table, kv_lens, free_pages, n_free, page_size: int, 
     if need and workspace is None:
         workspace = _new((need,), torch.uint8, dev, stream)
     tensors = (block_table, kv_lens, new_lens, do_append, release, free_pages, n_free, kv_lens_out, n_free_out, slots, granted)
-    _on_current_device(*tensors, workspace)
+    _on_current_device(stream, *tensors, workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     args = (ctypes.byref(p), *map(_ptr, tensors), _ptr(workspace), ws_bytes, _stream(stream))
     return BoundCall(lib.sdllm_paged_extend, args, (p, tensors, workspace), (slots, granted, kv_lens_out, n_free_out))
@@ -716,7 +718,7 @@ def bind_qk_norm_rope(q, k, positions, theta_base: float, q_weight=None, k_weigh
                          _DENSE if v is None else _strides(v, "v", keys, dtype), _strides(q_out, "q_out", heads, dtype),
                          _DENSE if k_out is None else _strides(k_out, "k_out", keys, dtype))
     tensors = (q, k, v, positions, q_weight, k_weight, q_out, k_out, k_pages, v_pages, slots)
-    _on_current_device(*tensors)
+    _on_current_device(stream, *tensors)
     args = (ctypes.byref(p), *map(_ptr, tensors), _stream(stream))
     return BoundCall(load_library().sdllm_qk_norm_rope, args, (p, tensors), (q_out, k_out))
 
@@ -740,7 +742,7 @@ def bind_paged_kv_append(k_pages, v_pages, k_blocks, v_blocks, slots, stream=Non
     _shaped(slots, "slots", (B, K), torch.int32)
     if L > 1 and (v_pages.stride(0) != k_pages.stride(0) or v_blocks.stride(0) != k_blocks.stride(0)):
         raise SdllmError(ERR_INVALID_ARG, "paged_kv_append: K and V tensors must share their layer strides")
-    _on_current_device(k_pages, v_pages, k_blocks, v_blocks, slots)
+    _on_current_device(stream, k_pages, v_pages, k_blocks, v_blocks, slots)
     p = PagedAppendParams(_dtype_code(k_pages), L, B, Hkv, D, K, page_size, n_pages, k_pages.stride(0) if L > 1 else 0,
                           k_blocks.stride(0) if L > 1 else 0)
     tensors = (k_pages, v_pages, k_blocks, v_blocks, slots)
@@ -795,7 +797,7 @@ def bind_paged_attention(q, k_pages, v_pages, block_table, kv_lens, max_kv_len: 
     if need and workspace is None:
         workspace = _new((need,), torch.uint8, q.device, stream)
     tensors = (q, k_pages, v_pages, block_table, kv_lens, k_block, v_block, q_lens, out)
-    _on_current_device(*tensors, workspace)
+    _on_current_device(stream, *tensors, workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     args = (ctypes.byref(p), *map(_ptr, tensors), _ptr(workspace), ws_bytes, _stream(stream))
     return BoundCall(load_library().sdllm_paged_attention, args, (p, tensors, workspace), out)
