@@ -33,7 +33,7 @@ template <int D, int RB> struct Rows {
   bf16x8 q[RB][NS];                                // MFMA B operands (lane: row l16, d = 32 s + 8 G .. + 7)
   f32x4 o[RB][NDB];
   float neg_m[RB];                                 // minus the reference of row l16
-  float thr[RB], lsum[RB];                         // thr kNegBig: no reference yet; lsum: RB == 1 the row's, else this lane's part
+  float thr[RB], lsum[RB];                         // thr kNegBig: no reference yet
   int pos[RB];                                     // position of row l16
 };
 
@@ -105,16 +105,10 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
       w.neg_m[rb] -= shift;
       w.thr[rb] = move ? h.thr8 : w.thr[rb];
     }
-    float ps = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = exp2_fast(sacc[rb][kb][e] * h.scale_log2);
-        sacc[rb][kb][e] = p;
-        if (RB != 1) ps += p;
-      }
-    if (RB != 1) w.lsum[rb] += ps;
+      for (int e = 0; e < 4; ++e) sacc[rb][kb][e] = exp2_fast(sacc[rb][kb][e] * h.scale_log2);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       union { uint32_t x[4]; s16x8 v; } cv;
@@ -125,14 +119,16 @@ __device__ __forceinline__ void compute_tile(const Hot& h, Rows<D, RB>& w, unsig
       pk[rb][u] = cv.v;
     }
   }
-  if (RB == 1) {                                   // row sums on the matrix pipe, as in the dense kernel
-    union { uint32_t x[4]; s16x8 v; } ones;
-    ones.x[0] = ones.x[1] = ones.x[2] = ones.x[3] = 0x3f803f80u;
-    f32x4 ls = {w.lsum[0], 0.f, 0.f, 0.f};
+  // row sums on the matrix pipe, from the rounded weights that the values are multiplied by
+  union { uint32_t x[4]; s16x8 v; } ones;
+  ones.x[0] = ones.x[1] = ones.x[2] = ones.x[3] = 0x3f803f80u;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    f32x4 ls = {w.lsum[rb], 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones.v), __builtin_bit_cast(bf16x8, pk[0][u]), ls, 0, 0, 0);
-    w.lsum[0] = ls[0];
+      ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones.v), __builtin_bit_cast(bf16x8, pk[rb][u]), ls, 0, 0, 0);
+    w.lsum[rb] = ls[0];
   }
   // ---- O^T += V^T P^T
 #pragma unroll
@@ -422,11 +418,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const long long slot0 = slot * a->R;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      float l = w.lsum[rb];
-      if (RB != 1) {
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-      }
+      const float l = w.lsum[rb];
       const int R = wave_row + 16 * rb + l16;
       if (R > last_row) continue;
       if (whole) {
