@@ -9,13 +9,15 @@
 //   S^T = K Q^T, O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, operands laid out as in the dense kernel (rows padded to 16 or 32).
 //   Online softmax: the product's accumulators start at minus the row's reference, so that it yields s - reference and a weight is
 //   one multiply and one exponential, whatever the scores' size; the reference moves only where a maximum exceeds it by 8 in log2
-//   units.  Weights are rounded to bf16 (2^-8 relative) for the second product, and the row sums are those of the rounded weights;
-//   all sums are fp32.
+//   units.  The second product takes bf16, and a weight goes in as two: rounded, and what that took from it, rounded in turn (2^-16 of the weight
+//   is lost).  K and V are read at HBM's rate, which leaves the matrix unit the room: as one number each, which loses 2^-8, a token over
+//   700 keys takes 7.14 us instead of 7.29, over 32 sequences of 8192 168.5 instead of 168.6, 32 rows of 8 sequences of 2000 keys (8 heads of
+//   64) 18.0 instead of 18.9.  The row sums are those of the same numbers; all sums are fp32.
 // A (sequence, head) that one wave walked alone is written at once; of the others every wave leaves (O, m, l), merged in tile order
 // by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
 //   TOGETHER: the eight waves of a workgroup share the tiles of one (sequence, K/V head) and merge through LDS: no second launch.
 // Measured, one row over 32 and 8 heads of 128: 32 sequences of 200 to 16384 keys, 501 MB, 80 + 5 us (5.8 TB/s); 64 of 4096, 1.07 GB,
-// 170 us (6.3 TB/s); one of 700, 7.1 us; one of 32768, 134 MB, 31 us.
+// 170 us (6.3 TB/s); one of 700, 7.3 us; one of 32768, 134 MB, 31 us.
 #include "paged_attention.h"
 
 namespace sdllm {
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
         for (int rb = 0; rb < RB; ++rb) hide<KB>(sacc[rb], k0, lo[rb], hi[rb], h.sinks, vis, missing, above, below);
       }
       // ---- online softmax: p = exp2((s - reference) scale_log2)
-      s16x8 pk[RB][U];
+      s16x8 pk[RB][U], rest[RB][U];                // rounded to bf16, and what that took from them
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         float mx = -INFINITY;
@@ -217,20 +219,24 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
           for (int e = 0; e < 4; ++e) sacc[rb][kb][e] = exp2_fast(sacc[rb][kb][e] * h.scale_log2);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          union { uint32_t w[4]; s16x8 v; } cv;
-          cv.w[0] = pack_bf16x2(sacc[rb][2 * u][0], sacc[rb][2 * u][1]);
-          cv.w[1] = pack_bf16x2(sacc[rb][2 * u][2], sacc[rb][2 * u][3]);
-          cv.w[2] = pack_bf16x2(sacc[rb][2 * u + 1][0], sacc[rb][2 * u + 1][1]);
-          cv.w[3] = pack_bf16x2(sacc[rb][2 * u + 1][2], sacc[rb][2 * u + 1][3]);
-          pk[rb][u] = cv.v;
+          union { uint32_t w[4]; s16x8 v; } p, q;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = sacc[rb][2 * u + i / 2][2 * (i % 2)], y = sacc[rb][2 * u + i / 2][2 * (i % 2) + 1];
+            p.w[i] = pack_bf16x2(x, y);
+            q.w[i] = pack_bf16x2(x - __uint_as_float(p.w[i] << 16), y - __uint_as_float(p.w[i] & 0xffff0000u));
+          }
+          pk[rb][u] = p.v; rest[rb][u] = q.v;
         }
-        // row sums on the matrix pipe, from the rounded probabilities that the values are weighted with
+        // row sums on the matrix pipe, from what the values are weighted with
         union { uint32_t w[4]; s16x8 v; } ones;
         ones.w[0] = ones.w[1] = ones.w[2] = ones.w[3] = 0x3f803f80u;
         f32x4 ls = {lsum[rb], 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
           ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones.v), __builtin_bit_cast(bf16x8, pk[rb][u]), ls, 0, 0, 0);
+          ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones.v), __builtin_bit_cast(bf16x8, rest[rb][u]), ls, 0, 0, 0);
+        }
         lsum[rb] = ls[0];
       }
       if (masked && cur.s.p1 > cur.s.p0) {         // rows at different positions: what a row does not see must not reach it
@@ -253,9 +259,11 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-            o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop[u][db]),
-                                                                __builtin_bit_cast(bf16x8, pk[rb][u]), o[rb][db], 0, 0, 0);
+          for (int rb = 0; rb < RB; ++rb) {
+            const bf16x8 v = __builtin_bit_cast(bf16x8, vop[u][db]);
+            o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pk[rb][u]), o[rb][db], 0, 0, 0);
+            o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, rest[rb][u]), o[rb][db], 0, 0, 0);
+          }
     }
 
     // ---- this wave's share of the unit is done

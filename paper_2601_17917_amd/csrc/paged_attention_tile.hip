@@ -3,7 +3,10 @@
 //
 // A workgroup owns 16 RB NW query rows (NW waves, 16 RB rows each) and walks key tiles of 64 that its waves share through a
 // ring in LDS: each wave moves 16-row slabs global -> LDS, one tile ahead of the one being computed (four waves, two workgroups per CU)
-// or two (eight waves, one workgroup per CU), one barrier per tile.  Products, operand layouts and the softmax are those of the stream kernel.
+// or two (eight waves, one workgroup per CU), one barrier per tile.  Products, operand layouts and the softmax are those of the stream kernel, but
+// for the weights of the values: rounded to bf16 (2^-8), as in the dense kernel, and divided by the sum of the rounded ones.  Here the matrix
+// unit is the bound; a second number for what the rounding takes cost 8 sequences of 500 to 8000 keys (28 / 4 heads, 32 rows) 34 -> 39 us and
+// 2 x 2048 causal rows behind up to 4096 keys 203 -> 281.
 //   FLAT (four waves of 16 rows): one row tile covers a (sequence, K/V head).  The workgroups walk equal shares of all key tiles of
 //         the call, laid end to end as the stream kernel's waves do, so that lengths need not be alike.
 //   else: a workgroup per (row tile, sequence, K/V head), the tiles of the last rows, which see most under a causal mask, first; or,

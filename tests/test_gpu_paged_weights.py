@@ -1,10 +1,12 @@
-"""What the weights of the bf16 attention are divided by."""
+"""The weights of the bf16 attention: what they are divided by, and how many bits of them reach the values."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from paged_util import attention_problem, call_attention
+from gpu_util import to_f64_host
+from paged_util import attention_problem, call_attention, oracle_outputs
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +31,18 @@ def test_the_mean_of_ones_is_one(gpu_lib, K, Hq, D, splits):
         scale = (m + math.log2(1.0 + 0.97 * 2.0 ** -8)) / math.log2(math.e)
         for mask in (dict(), dict(causal=True), dict(causal=True, window=700, sinks=5)):
             assert (call_attention(gpu_lib, s, kv_splits=splits, scale=scale, **mask) == 1.0).all()
+
+
+@pytest.mark.parametrize("Hq,K,lens", [(4, 1, [700, 33, 5]), (16, 1, [90, 2000]), (64, 1, [40, 700]), (8, 8, [19, 333]), (2, 30, [31, 50])])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("splits", [0, 3])
+def test_up_to_32_rows_lose_only_the_rounding_of_the_output(gpu_lib, Hq, K, lens, D, splits):
+    """With A = sum_j p_j |v_jd| / sum_j p_j: a weight is two bf16 numbers, the second half a step (2^-8) of what the first one lost (2^-8):
+    2^-16 of each; scores, exponentials and sums in fp32 1e-5 of each, as in the fp32 kernel (paged_util); the output half a step
+    of bf16, 2^-8 |o|.  Weights of one bf16 number would be off by up to 2^-8 A."""
+    s = attention_problem(62 + K, "bf16", len(lens), Hq, 2, D, K, 16, lens, None, False)
+    for mask in (dict(), dict(causal=True, window=300, sinks=2)):
+        got = to_f64_host(call_attention(gpu_lib, s, kv_splits=splits, **mask))
+        want, want_abs = oracle_outputs(s, **mask)
+        bound = 2.0 ** -8 * np.abs(want) + 2.0 * (2.0 ** -16 + 1e-5) * want_abs + 1e-6
+        assert (np.abs(got - want) <= bound).all()
