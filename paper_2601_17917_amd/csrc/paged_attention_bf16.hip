@@ -9,15 +9,16 @@
 //   S^T = K Q^T, O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, operands laid out as in the dense kernel (rows padded to 16 or 32).
 //   Online softmax: the product's accumulators start at minus the row's reference, so that it yields s - reference and a weight is
 //   one multiply and one exponential, whatever the scores' size; the reference moves only where a maximum exceeds it by 8 in log2
-//   units.  The second product takes bf16, and a weight goes in as two: rounded, and what that took from it, rounded in turn (2^-16 of the weight
-//   is lost).  K and V are read at HBM's rate, which leaves the matrix unit the room: as one number each, which loses 2^-8, a token over
-//   700 keys takes 7.14 us instead of 7.29, over 32 sequences of 8192 168.5 instead of 168.6, 32 rows of 8 sequences of 2000 keys (8 heads of
-//   64) 18.0 instead of 18.9.  The row sums are those of the same numbers; all sums are fp32.
+//   units.  The second product takes bf16, and a weight goes in as two: the next number below it, and what is missing, rounded (2^-15 of the
+//   weight is lost at most).  Neither is negative or, down to weights of 2^-100, zero: infinite values keep their sign.  K and V are read at
+//   HBM's rate, which leaves the matrix unit the room: as one number each, which loses 2^-8, a token over 700 keys takes 7.16 us instead of 7.4,
+//   over 32 sequences of 8192 168.0 instead of 168.4, 32 rows of 8 sequences of 2000 keys (8 heads of 64) 17.9 instead of 18.9.  The row sums
+//   are those of the same numbers; all sums are fp32.
 // A (sequence, head) that one wave walked alone is written at once; of the others every wave leaves (O, m, l), merged in tile order
 // by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
 //   TOGETHER: the eight waves of a workgroup share the tiles of one (sequence, K/V head) and merge through LDS: no second launch.
 // Measured, one row over 32 and 8 heads of 128: 32 sequences of 200 to 16384 keys, 501 MB, 80 + 5 us (5.8 TB/s); 64 of 4096, 1.07 GB,
-// 170 us (6.3 TB/s); one of 700, 7.3 us; one of 32768, 134 MB, 31 us.
+// 170 us (6.3 TB/s); one of 700, 7.4 us; one of 32768, 134 MB, 31 us.
 #include "paged_attention.h"
 
 namespace sdllm {
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
         for (int rb = 0; rb < RB; ++rb) hide<KB>(sacc[rb], k0, lo[rb], hi[rb], h.sinks, vis, missing, above, below);
       }
       // ---- online softmax: p = exp2((s - reference) scale_log2)
-      s16x8 pk[RB][U], rest[RB][U];                // rounded to bf16, and what that took from them
+      s16x8 pk[RB][U], rest[RB][U];                // the next bf16 number below, and what is missing: both positive
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         float mx = -INFINITY;
@@ -223,8 +224,9 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float x = sacc[rb][2 * u + i / 2][2 * (i % 2)], y = sacc[rb][2 * u + i / 2][2 * (i % 2) + 1];
-            p.w[i] = pack_bf16x2(x, y);
-            q.w[i] = pack_bf16x2(x - __uint_as_float(p.w[i] << 16), y - __uint_as_float(p.w[i] & 0xffff0000u));
+            const unsigned x1 = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u), y1 = __builtin_elementwise_sub_sat(__float_as_uint(y), 1u);
+            p.w[i] = __builtin_amdgcn_perm(y1, x1, 0x07060302);               // their upper halves
+            q.w[i] = pack_bf16x2(x - __uint_as_float(x1 & 0xffff0000u), y - __uint_as_float(y1 & 0xffff0000u));
           }
           pk[rb][u] = p.v; rest[rb][u] = q.v;
         }
