@@ -139,7 +139,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
 #pragma unroll
       for (int db = 0; db < NDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    bool redo = false;
+    bool taken = false;
     int i = begin;
     for (; i < cur.T && left > 0; ++i, --left) {
       const unsigned long long vis = vis_next;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
 #pragma unroll
           for (int db = 0; db < NDB; ++db) bad |= nonfinite_bits(__builtin_bit_cast(u32x4, vop[u][db]));
         if (__builtin_expect(__ballot(bad != 0) != 0, 0)) {
-          redo = true;
+          taken = true;
 #pragma unroll
           for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_stream_kernel(P
         if (G == 0) { part_ml[2 * R] = thr[rb] == kNegBig ? kNegBig : -neg_m[rb][0]; part_ml[2 * R + 1] = lsum[rb]; }
       }
     }
-    if (redo) redo_rows<uint16_t, D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, part_o, part_ml);
+    if (taken) put_back<uint16_t, D, TK>(cur.s, cur.b, cur.kvh, begin, i, 0, 16 * RB, whole, part_o);
     if constexpr (TOGETHER) {
       if (waves > 1) {
         __syncthreads();

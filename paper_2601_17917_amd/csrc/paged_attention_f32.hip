@@ -130,7 +130,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_f32_kernel(Page
         }
       }
     };
-    bool redo = false;
+    bool taken = false;
     int i = begin;
     unsigned vis_next = load_k(i);
     for (; i < cur.T && left > 0; ++i, --left) {
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_f32_kernel(Page
 #pragma unroll
               for (int e = 0; e < 4; ++e) bad |= !__builtin_isfinite(v[r][c][e]);
           if (__builtin_expect(__ballot(bad) != 0, 0)) {
-            redo = true;
+            taken = true;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(TOGETHER ? 512 : 256, 2) void paged_f32_kernel(Page
             *reinterpret_cast<f32x4*>(to + 64 * c + 16 * G + 4 * e) = f32x4{o[c][0][e], o[c][1][e], o[c][2][e], o[c][3][e]} * inv;
         if (!whole && G == 0) { part_ml[2 * R] = m; part_ml[2 * R + 1] = lsum; }
       }
-      if (redo) redo_rows<float, D, TK>(cur.s, cur.b, cur.kvh, begin, i, row0, 16, whole, part_o, part_ml);
+      if (taken) put_back<float, D, TK>(cur.s, cur.b, cur.kvh, begin, i, row0, 16, whole, part_o);
       if constexpr (TOGETHER) {
         if (waves > 1) {
           __syncthreads();

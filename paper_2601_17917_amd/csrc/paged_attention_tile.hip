@@ -369,7 +369,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       wg_lo = a->window > 0 ? cur.s.p1 - a->window + 1 : 0;
     }
     if (NST > 2) wait_transfers();                 // the query rows: no wait for them is left to the loop
-    bool redo = false;
+    bool taken = false;
     int i = begin;
     while (i < cur.T && left > 0) {
       // The tile has landed: transfers complete in order, and behind it at most those of one whole tile are in flight
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       wait_lds();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (border) redo |= uniform(*flag) >= number;
+      if (border) taken |= uniform(*flag) >= number;
       const unsigned long long seen = vis[0];
       if (NST > 2) vis[0] = vis[NST - 2];
       if (left > NST - 1) {
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (G == 0) { a->ws_ml[2 * (slot0 + R)] = w.thr[rb] == kNegBig ? kNegBig : -w.neg_m[rb]; a->ws_ml[2 * (slot0 + R) + 1] = l; }
       }
     }
-    if (redo) redo_rows<uint16_t, D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, a->ws_o + slot0 * D, a->ws_ml + 2 * slot0);
+    if (taken) put_back<uint16_t, D, kTK>(cur.s, cur.b, cur.kvh, begin, i, wave_row, WROWS, whole, a->ws_o + slot0 * D);
     if (FLAT) {
       slot = 2LL * blockIdx.x + 1;                 // the first unit's partial result goes to slot 0, the last's to 1
       if (left > 0) { cur.i = cur.T - 1; next_tile<kTK>(cur); }
