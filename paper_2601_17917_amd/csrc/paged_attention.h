@@ -558,8 +558,9 @@ __device__ __forceinline__ RowSum add_up(Args a, int first, int last, Slot&& slo
   return s;
 }
 // Rows up to which each has a workgroup of its own for that: that many are on the chip at once, and what counts is the way through a
-// row's shares.  With more rows it is the number of workgroups.  (32 query heads, one row each, over 32768 keys: 35 us with the
-// attention itself, 67 with all rows in 128 workgroups; 28 heads of 32 rows for 8 sequences of 4096 keys: 55 and 48.)
+// row's shares.  With more rows it is the number of workgroups.  (us with the attention itself, alone and in workgroups of eight rows, heads
+// of 128: 32 rows, one sequence of 32768 keys 31 and 46; 2048 rows, 8 of 4096 36 and 35; 4096 rows, 16 of 4096 58 and 54; 8192 rows, 32 of
+// 4096 102 and 93.)
 constexpr int kMergeAlone = 8 * kNumCUs;
 
 // Kernels: bf16 by query rows per (sequence, K/V head), up to 32 (stream) and more (tile); fp32

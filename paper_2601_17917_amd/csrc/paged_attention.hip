@@ -121,13 +121,6 @@ size_t paged_attention_workspace_bytes(const sdllm_paged_attn_params& p, bool wi
   return few_rows(p) ? paged_stream_workspace_bytes(p, with_block) : paged_tile_workspace_bytes(p, with_block);
 }
 
-static void dense_or(const int64_t* given, int H, int K, int D, long long* out) {
-  const bool dense = given[0] == 0 && given[1] == 0 && given[2] == 0;
-  out[0] = dense ? (long long)H * K * D : given[0];
-  out[1] = dense ? (long long)K * D : given[1];
-  out[2] = dense ? D : given[2];
-}
-
 hipError_t launch_paged_attention(const sdllm_paged_attn_params& p, const void* q, const void* k_pages, const void* v_pages,
                                   const int32_t* table, const int32_t* lens, const void* k_block, const void* v_block,
                                   const int32_t* q_lens, void* out, void* workspace, hipStream_t stream) {

@@ -11,14 +11,14 @@
 //   one multiply and one exponential, whatever the scores' size; the reference moves only where a maximum exceeds it by 8 in log2
 //   units.  The second product takes bf16, and a weight goes in as two: the next number below it, and what is missing, rounded (2^-15 of the
 //   weight is lost at most).  Neither is negative or, down to weights of 2^-100, zero: infinite values keep their sign.  K and V are read at
-//   HBM's rate, which leaves the matrix unit the room: as one number each, which loses 2^-8, a token over 700 keys takes 7.16 us instead of 7.4,
+//   HBM's rate, which leaves the matrix unit the room: as one number each, which loses 2^-8, a token over 700 keys takes 7.1 us instead of 7.3,
 //   over 32 sequences of 8192 168.0 instead of 168.4, 32 rows of 8 sequences of 2000 keys (8 heads of 64) 17.9 instead of 18.9.  The row sums
 //   are those of the same numbers; all sums are fp32.
 // A (sequence, head) that one wave walked alone is written at once; of the others every wave leaves (O, m, l), merged in tile order
 // by a second launch.  Which wave does what follows from the lengths alone: no atomics, the same result every time.
 //   TOGETHER: the eight waves of a workgroup share the tiles of one (sequence, K/V head) and merge through LDS: no second launch.
-// Measured, one row over 32 and 8 heads of 128: 32 sequences of 200 to 16384 keys, 501 MB, 80 + 5 us (5.8 TB/s); 64 of 4096, 1.07 GB,
-// 170 us (6.3 TB/s); one of 700, 7.4 us; one of 32768, 134 MB, 31 us.
+// Measured, one row over 32 and 8 heads of 128: 32 sequences of 200 to 16384 keys, 501 MB, 80 + 5 us (5.9 TB/s); 64 of 4096, 1.07 GB,
+// 168 us (6.4 TB/s); one of 700, 7.3 us; one of 32768, 134 MB, 31 us.
 #include "paged_attention.h"
 
 namespace sdllm {

@@ -12,8 +12,8 @@
 //   else: a workgroup per (row tile, sequence, K/V head), the tiles of the last rows, which see most under a causal mask, first; or,
 //         where that is fewer than fit on the chip, per (row tile, sequence, K/V head, part of the keys).  Sequences get parts by their
 //         lengths: parts have as few tiles as let all workgroups be on the chip at once.
-// Many rows are bound by the matrix cores and the softmax between them: 8 x 512 rows of 32 / 8 heads over 4096 keys 255 us (1.08
-// PFLOP/s), 2 x 2048 causal rows behind 4096 keys 307 us (1.12).  Blocks, 28 and 4 heads of 32 rows, 8 sequences of 500 to 8000 keys: 28 us
+// Many rows are bound by the matrix cores and the softmax between them: 8 x 512 rows of 32 / 8 heads over 4096 keys 250 us (1.10
+// PFLOP/s), 2 x 2048 causal rows behind 4096 keys 303 us (1.13).  Blocks, 28 and 4 heads of 32 rows, 8 sequences of 500 to 8000 keys: 27 us
 // and 8 us in the merge, of which a workgroup's start (its place, table, queries, the first two tiles) and end are 10.
 #include "paged_attention.h"
 #include <algorithm>

@@ -6,8 +6,9 @@
 
 namespace sdllm {
 
-// Division of n < 2^31 by a constant 1 <= d < 2^31 with one high multiply (the round-up method: m = ceil(2^32 (2^s - d) / d),
-// s = ceil(log2 d), q = (mulhi(n, m) + n) >> s; the sum stays below 2^32 because mulhi(n, m) <= n).
+// Division of n < 2^31 by a constant 1 <= d < 2^31 with one high multiply (the round-up method of Granlund and Montgomery,
+// "Division by invariant integers using multiplication", 1994: m = ceil(2^32 (2^s - d) / d), s = ceil(log2 d),
+// q = (mulhi(n, m) + n) >> s; the sum stays below 2^32 because mulhi(n, m) <= n).
 struct FastDiv {
   unsigned d = 1, m = 0, s = 0;
   FastDiv() = default;
@@ -28,6 +29,14 @@ __device__ __forceinline__ int wave_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
   v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15, 31: and over them
   return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+}
+
+// Strides of a tensor [B, H, K, D] as given, or the dense one's
+inline void dense_or(const int64_t* given, int H, int K, int D, long long* out) {
+  const bool dense = given[0] == 0 && given[1] == 0 && given[2] == 0;
+  out[0] = dense ? (long long)H * K * D : given[0];
+  out[1] = dense ? (long long)K * D : given[1];
+  out[2] = dense ? D : given[2];
 }
 
 // Errors of entry points that live outside api.hip end up in the same per-thread text (sdllm_last_error)

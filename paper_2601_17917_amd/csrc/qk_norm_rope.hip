@@ -7,8 +7,8 @@
 // turns, position * f_i / 2 pi, in double (its fraction is what counts, and float loses it beyond a few thousand positions), the
 // fraction's sine and cosine in float.  A lane holds two 16-byte vectors of a row that contain whole pairs -- (i, i + R/2) as a
 // vector of the first half and the matching one of the second, or adjacent vectors -- so that the rotation needs no exchange
-// between lanes; the sum of squares is reduced over the 4 to 32 lanes of a row.  Several tokens for a workgroup were slower (36 to 42
-// us for 2 x 4096 tokens of 36 heads of 128, 4.9 TB/s and 31 us this way).
+// between lanes; the sum of squares is reduced over the 4 to 32 lanes of a row.  2 x 4096 tokens of 36 heads of 128, 151 MB,
+// take 25 us (6.1 TB/s); several tokens for a workgroup were slower (36 to 42 where one each took 33, before outputs went past L2).
 #include "paged_common.h"
 #include <cmath>
 
@@ -162,13 +162,6 @@ static void launch_gl(const NormRopeArgs& a, bool interleaved, bool streaming, d
   }
 }
 
-static void dense_or(const int64_t* given, int H, int K, int D, long long* out) {
-  const bool dense = given[0] == 0 && given[1] == 0 && given[2] == 0;
-  out[0] = dense ? (long long)H * K * D : given[0];
-  out[1] = dense ? (long long)K * D : given[1];
-  out[2] = dense ? D : given[2];
-}
-
 hipError_t launch_qk_norm_rope(const sdllm_qk_norm_rope_params& p, const void* q, const void* k, const void* v,
                                const int32_t* positions, const void* q_weight, const void* k_weight, void* q_out, void* k_out,
                                void* k_pages, void* v_pages, const int32_t* slots, hipStream_t stream) {
@@ -183,8 +176,8 @@ hipError_t launch_qk_norm_rope(const sdllm_qk_norm_rope_params& p, const void* q
   a.K = p.K; a.Hq = p.Hq; a.Hkv = p.Hkv; a.D = p.D; a.R = p.rotary_dim; a.per_row = p.positions_per_row;
   a.shift = slots ? __builtin_ctz(p.page_size) : 0;
   a.slots_total = slots ? p.n_pages << a.shift : 0;
-  // What is more than the L2s hold is not kept there for the reader.  (2 x 4096 tokens of 36 heads of 128: 31.1 us, against 33.0 through
-  // L2; 2 x 4000 of 48 heads of 64: 18.7, 25.3.)
+  // What is more than the L2s hold is not kept there for the reader.  (Three sets of tensors in turn, past L2
+  // and through it: 2 x 4096 tokens of 36 heads of 128 26.6 us and 33.8, 2 x 4000 of 48 heads of 64 18.6 and 24.3.)
   const bool streaming = (double)p.B * p.K * (p.Hq + p.Hkv * (slots ? 2 : 1)) * p.D * (p.dtype == SDLLM_FP32 ? 4 : 2) > 32e6;
   a.eps = p.eps; a.amplitude = p.amplitude;
   a.rows = p.Hq + p.Hkv * (slots ? 2 : 1);
