@@ -143,6 +143,7 @@ int sdllm_paged_kv_append(const sdllm_paged_append_params* p,
  *     p - j < window or j < sinks      (window > 0: a sliding window, with the first `sinks` keys kept visible)
  * and its page id is valid.  out row = softmax over the visible keys of scale * q k, times their values; a row that sees no
  * key is zero, and what is stored for hidden keys, or behind the last one in a page, does not matter, NaN included.
+ * A value of a visible key that is infinite or NaN reaches its column of the rows that see it, and nothing else.
  * One token per sequence (K = 1), the rows of a block and the pieces of prompts are the same call.
  *
  *   B, Hq, Hkv, D   as for sdllm_block_attention; D in {64, 128} for both dtypes; B * Hkv < 2^22,
